@@ -208,6 +208,169 @@ COMET_API comet_status_t comet_kv4_dequantize(const uint8_t* codes, const uint16
                                               uint16_t* out, int T, int C, int G,
                                               hipStream_t stream);
 
+/* ---- between the qkv and the o product: positions, paged cache, attention ----
+ *
+ * Rotary positions.  X and out are device fp16, rows of `heads` heads of
+ * head_dim channels, row m at element m * x_stride (out_stride); a row of a
+ * wider buffer (the q and k heads of a qkv output) is addressed by its first
+ * channel and the buffer's row length.  out == X (and out_stride == x_stride)
+ * rotates in place; otherwise the two must not overlap.  With
+ * theta_i = positions[m] * freqs[i] (64 bits) and i < rot_dim / 2,
+ *     out_a = X_a c - X_b s,  out_b = X_b c + X_a s,
+ *     c = mscale cos(theta_i),  s = mscale sin(theta_i)      (32 bits)
+ * for the channels (a, b) = (i, i + rot_dim / 2) of every head, or, with
+ * interleaved != 0, (2i, 2i + 1); channels from rot_dim on are copied (left
+ * alone in place).
+ *   positions  device int32 [M], any values.
+ *   freqs      device float64 [rot_dim / 2], radians per position
+ *              (comet_rope_frequencies makes them on the host).
+ * rot_dim even, 2 <= rot_dim <= head_dim <= 1024; strides >= heads * head_dim;
+ * mscale finite; M and heads at most 2,097,120 and 65,535
+ * (COMET_ERR_UNSUPPORTED beyond).  X and out need only the alignment of fp16,
+ * positions of int32, freqs of float64 (16-byte aligned rows with rot_dim a
+ * multiple of 16 are faster). */
+COMET_API comet_status_t comet_rope(const uint16_t* X, const int32_t* positions,
+                                    const double* freqs, uint16_t* out, int M, int heads,
+                                    int head_dim, int rot_dim, int x_stride, int out_stride,
+                                    int interleaved, float mscale, hipStream_t stream);
+
+/* How comet_rope_frequencies stretches the positions of a longer context.  With
+ * f_i = base^(-2i / rot_dim) and factor >= 1:
+ *   NONE    f_i
+ *   LINEAR  f_i / factor (position interpolation)
+ *   BASE    base' = base * factor^(rot_dim / (rot_dim - 2)): the slowest pair is
+ *           slowed `factor` times, the fastest not at all (rot_dim > 2)
+ *   BANDS   by the number of turns n_i = original_len * f_i / (2 pi) that a pair
+ *           makes over the original context: f_i / factor up to n_i = low, f_i
+ *           from n_i = high on, and in between f_i ((1 - t) / factor + t) with
+ *           t = (n_i - low) / (high - low)
+ *   RAMP    the same blend over pair indexes: t falls from 1 to 0 between the
+ *           pairs floor(i(high)) and ceil(i(low)) (clamped to 0 .. rot_dim - 1,
+ *           0.001 apart at least), where i(n) = rot_dim ln(original_len / (2 pi n))
+ *           / (2 ln base) is where a pair makes n turns; *mscale =
+ *           0.1 ln(factor) + 1 (1 for the others) (arXiv 2309.00071). */
+typedef enum {
+  COMET_ROPE_NONE = 0,
+  COMET_ROPE_LINEAR = 1,
+  COMET_ROPE_BASE = 2,
+  COMET_ROPE_BANDS = 3,
+  COMET_ROPE_RAMP = 4
+} comet_rope_scaling_t;
+
+/* Host only (nothing is launched): freqs [rot_dim / 2] float64 and *mscale (may
+ * be NULL) for comet_rope.  base > 1; factor, low, high and original_len are
+ * read where the scaling names them: factor >= 1, 0 < low < high,
+ * original_len >= 1, all finite. */
+COMET_API comet_status_t comet_rope_frequencies(double* freqs, int rot_dim, double base,
+                                                int scaling, double factor, double low,
+                                                double high, double original_len,
+                                                float* mscale);
+
+/* A paged 4-bit K/V cache: num_pages pages of page_size tokens.  The device
+ * buffers are the caller's; the struct is read during a call and not retained.
+ *   codes   uint8 [num_pages][kv_heads][page_size][head_dim / 2]
+ *   params  fp16  [num_pages][kv_heads][page_size][head_dim / G][2]
+ * A row of one token and head has the codes and {s, mn} that
+ * comet_kv4_quantize gives it (groups of G channels), so comet_kv4_dequantize
+ * reads pages with T = rows, C = head_dim.
+ * page_size a power of two, 16 .. 1024; head_dim 64 or 128; G 32, 64 or 128, at
+ * most head_dim; kv_heads at most 1024; num_pages >= 1 (any number that fits the
+ * memory).  All four buffers 16-byte aligned. */
+typedef struct {
+  uint8_t* k_codes;
+  uint16_t* k_params;
+  uint8_t* v_codes;
+  uint16_t* v_params;
+  int num_pages;
+  int page_size;
+  int kv_heads;
+  int head_dim;
+  int G;
+} comet_kv4_cache_t;
+
+/* A ragged batch: B sequences, whose rows lie one after another in buffers of M
+ * rows.  The device arrays are read when the work runs, so a captured call can
+ * be replayed with new contents.
+ *   row_start    device int32 [B + 1], ascending: rows row_start[b] ..
+ *                row_start[b + 1] - 1 are sequence b's (none: an idle
+ *                sequence).  Rows in no sequence are neither read nor written.
+ *   seq_lens     device int32 [B]: L_b, tokens of sequence b, the rows of this
+ *                call included: row i of n_b is at position L_b - n_b + i.
+ *                Rows at negative positions have no token.
+ *   block_table  device int32 [B][max_pages]: token j of sequence b lies at
+ *                slot j % page_size of page block_table[b][j / page_size].
+ *                Entries outside [0, num_pages) and tokens from max_pages *
+ *                page_size on are holes: nothing is stored there, they read as
+ *                zeros, and no row attends to them.
+ *   max_rows     host: no sequence has more rows (M if unknown); a sequence
+ *                with more has unspecified outputs.
+ * No content of these arrays makes a call leave the cache or the row buffers.
+ * 4-byte aligned.  B at most 65,536, M at most 2,097,120, max_pages * page_size
+ * at most 2^30 (COMET_ERR_UNSUPPORTED beyond). */
+typedef struct {
+  const int32_t* row_start;
+  const int32_t* seq_lens;
+  const int32_t* block_table;
+  int B;
+  int M;
+  int max_pages;
+  int max_rows;
+} comet_kv4_batch_t;
+
+/* Quantizes the rows of a batch into its cache: row i of sequence b to the
+ * token at its position.  K and V: device fp16, rows of kv_heads heads of
+ * head_dim channels, row m at element m * k_stride (v_stride); 16-byte aligned,
+ * strides multiples of 8 and at least kv_heads * head_dim.  Bit-exact with
+ * comet_kv4_quantize row by row; non-finite inputs are not supported.  Two rows
+ * of one call must not have the same place (sequences may share pages that
+ * neither writes). */
+COMET_API comet_status_t comet_kv4_append(const comet_kv4_cache_t* cache,
+                                          const comet_kv4_batch_t* batch, const uint16_t* K,
+                                          const uint16_t* V, int k_stride, int v_stride,
+                                          hipStream_t stream);
+
+/* The reverse: row i of sequence b becomes the fp16 values (those of
+ * comet_kv4_dequantize) of the token at its position, zeros where there is
+ * none.  K or V may be NULL (not read back); alignment and strides as above. */
+COMET_API comet_status_t comet_kv4_gather(const comet_kv4_cache_t* cache,
+                                          const comet_kv4_batch_t* batch, uint16_t* K,
+                                          uint16_t* V, int k_stride, int v_stride,
+                                          hipStream_t stream);
+
+/* Causal attention of a batch's rows over the cache (which holds their own
+ * tokens too): row i of sequence b, at position p, head h of `heads`, sees the
+ * tokens j <= p of sequence b that are no holes, with window > 0 only those with
+ * j > p - window, and
+ *     out = sum_j w_j v_j / sum_j w_j,  w_j = exp(scale * q . k_j),
+ * with the k_j and v_j of kv head h / (heads / kv_heads) as q * s + mn of their
+ * codes, without the rounding to fp16 of comet_kv4_dequantize.  A row that sees
+ * no token is zeros.  Products are exact to fp16 inputs (the weights w_j are
+ * rounded to fp16, relative to the largest), sums are fp32, the output is
+ * rounded once.  What a row does not see has no influence on it, not-a-number
+ * included.  Deterministic for a given build, device and batch.
+ *   Q, out     device fp16, rows of `heads` heads of head_dim channels, row m at
+ *              element m * q_stride (out_stride); 16-byte aligned, strides
+ *              multiples of 8 and at least heads * head_dim; no overlap.
+ *   workspace  device, comet_kv4_attention_workspace(...) bytes, 16-byte aligned
+ *              (NULL where that is 0): the caller's, for the partial results of
+ *              long contexts, needing no initial content and holding none
+ *              between calls.  Calls that may overlap need one each.
+ * heads a multiple of kv_heads, at most 1024; scale finite; window >= 0 (0: no
+ * limit). */
+COMET_API comet_status_t comet_kv4_attention(const comet_kv4_cache_t* cache,
+                                             const comet_kv4_batch_t* batch, const uint16_t* Q,
+                                             uint16_t* out, int heads, int q_stride,
+                                             int out_stride, float scale, int window,
+                                             void* workspace, size_t workspace_bytes,
+                                             hipStream_t stream);
+
+/* Host only: bytes of workspace comet_kv4_attention needs for this cache, batch
+ * (its sizes; the arrays are not read) and number of heads on a device with
+ * `num_cus` compute units, or 0 where it needs none or the sizes are refused. */
+COMET_API size_t comet_kv4_attention_workspace(const comet_kv4_cache_t* cache,
+                                               const comet_kv4_batch_t* batch, int heads,
+                                               int num_cus);
+
 /* W4Ax GEMM (Sec. 4, O = WX): out[m][n] = fp16( sum_g a_scales[g][m] *
  * w_scales[g][n] * sum_{c<G} qa[m][gG+c] * qw[n][gG+c] ).  The per-block sums
  * are exact; the sum over blocks is fp32 in an unspecified order, rounded once

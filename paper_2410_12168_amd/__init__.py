@@ -7,8 +7,10 @@ streams.  There is no CPU fallback: if libcomet.so is missing and cannot be
 built, importing a function raises.
 
 Convenience wrappers (``quantize_act``, ``pack_w4``, ``w4ax_gemm``,
-``channel_absmax``, ``plan_channel_perm``, ``kv4_quantize``, ``kv4_dequantize``)
-allocate the outputs with ``torch.empty`` and call the same entry points.
+``channel_absmax``, ``plan_channel_perm``, ``kv4_quantize``, ``kv4_dequantize``,
+``rope``, ``kv4_append``, ``kv4_gather``, ``kv4_attention``) allocate the outputs
+with ``torch.empty`` and call the same entry points.  ``KV4Cache`` and
+``KV4Batch`` hold what the calls on the paged cache share.
 """
 from __future__ import annotations
 
@@ -73,6 +75,12 @@ def lib():
         "comet_kv4_dequantize": (I, [P, P, P, I, I, I, P]),
         "comet_w4ax_gemm_swiglu_quant": (I, [P, P, P, P, P, I, I, I, I, P, P, P, P]),
         "comet_swiglu_quantize": (I, [P, P, P, P, I, I, I, P]),
+        "comet_rope": (I, [P, P, P, P, I, I, I, I, I, I, I, ctypes.c_float, P]),
+        "comet_rope_frequencies": (I, [P, I, ctypes.c_double, I] + [ctypes.c_double] * 4 + [P]),
+        "comet_kv4_append": (I, [P, P, P, P, I, I, P]),
+        "comet_kv4_gather": (I, [P, P, P, P, I, I, P]),
+        "comet_kv4_attention": (I, [P, P, P, P, I, I, I, ctypes.c_float, I, P, S, P]),
+        "comet_kv4_attention_workspace": (S, [P, P, I, I]),
         "comet_gemm_kernel": (I, [I, I, I, I, I]),
         "comet_w4ax_gemm_noalloc": (I, [P, P, P, P, P, P, I, I, I, I, P]),
         "comet_build_stamp": (ctypes.c_char_p, []),
@@ -289,6 +297,107 @@ def comet_kv4_dequantize(codes, params, out, T: int, C: int, G: int = 128, strea
                                       _stream(stream)))
 
 
+ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "bands": 3, "ramp": 4}
+
+
+def comet_rope(X, positions, freqs, out, M: int, heads: int, head_dim: int, rot_dim: int,
+               x_stride: int, out_stride: int, interleaved: bool = False, mscale: float = 1.0,
+               stream=None) -> None:
+    if M > 0 and heads > 0:
+        _row_room(X, M, x_stride, heads * head_dim, "X")
+        _room(positions, 4 * M, "positions")
+        _room(freqs, 4 * rot_dim, "freqs")
+        _row_room(out, M, out_stride, heads * head_dim, "out")
+    _check(lib().comet_rope(_ptr(X), _ptr(positions), _ptr(freqs), _ptr(out), M, heads, head_dim,
+                            rot_dim, x_stride, out_stride, int(bool(interleaved)), mscale,
+                            _stream(stream)))
+
+
+def comet_rope_frequencies(freqs, rot_dim: int, base: float, scaling: int, factor: float,
+                           low: float, high: float, original_len: float, mscale=None) -> None:
+    """Host-only: freqs (and mscale) are host numpy arrays, float64 and float32."""
+    _room(freqs, 4 * rot_dim, "freqs")
+    _room(mscale, 4, "mscale")
+    _check(lib().comet_rope_frequencies(_ptr(freqs), rot_dim, base, scaling, factor, low, high,
+                                        original_len, _ptr(mscale)))
+
+
+class KV4CacheStruct(ctypes.Structure):
+    """comet_kv4_cache_t"""
+
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k_codes", "k_params", "v_codes", "v_params")] + [
+        (n, ctypes.c_int) for n in ("num_pages", "page_size", "kv_heads", "head_dim", "G")]
+
+
+class KV4BatchStruct(ctypes.Structure):
+    """comet_kv4_batch_t"""
+
+    _fields_ = [(n, ctypes.c_void_p) for n in ("row_start", "seq_lens", "block_table")] + [
+        (n, ctypes.c_int) for n in ("B", "M", "max_pages", "max_rows")]
+
+
+def _row_room(t, M: int, stride: int, width: int, name: str) -> None:
+    """A tensor of fp16 rows must reach, from its first element to the end of its
+    storage, over M rows of `width` elements, `stride` apart."""
+    if t is None or isinstance(t, int):
+        return
+    have = t.nbytes if isinstance(t, np.ndarray) else (
+        t.untyped_storage().nbytes() - t.storage_offset() * t.element_size())
+    need = 2 * ((M - 1) * stride + width)
+    if have < need:
+        raise ValueError(f"{name}: {have} bytes, the call needs {need}")
+
+
+def _struct(s):
+    """A KV4Cache or KV4Batch as the address of its struct (None stays null)."""
+    if s is None:
+        return None
+    return ctypes.addressof(s.struct if hasattr(s, "struct") else s)
+
+
+def _kv4_row_room(cache, batch, K, V, k_stride: int, v_stride: int) -> None:
+    if cache is None or batch is None:
+        return
+    c, b = getattr(cache, "struct", cache), getattr(batch, "struct", batch)
+    if b.M > 0 and c.kv_heads > 0:
+        _row_room(K, b.M, k_stride, c.kv_heads * c.head_dim, "K")
+        _row_room(V, b.M, v_stride, c.kv_heads * c.head_dim, "V")
+
+
+def comet_kv4_append(cache, batch, K, V, k_stride: int, v_stride: int, stream=None) -> None:
+    _kv4_row_room(cache, batch, K, V, k_stride, v_stride)
+    _check(lib().comet_kv4_append(_struct(cache), _struct(batch), _ptr(K), _ptr(V), k_stride,
+                                  v_stride, _stream(stream)))
+
+
+def comet_kv4_gather(cache, batch, K, V, k_stride: int, v_stride: int, stream=None) -> None:
+    _kv4_row_room(cache, batch, K, V, k_stride, v_stride)
+    _check(lib().comet_kv4_gather(_struct(cache), _struct(batch), _ptr(K), _ptr(V), k_stride,
+                                  v_stride, _stream(stream)))
+
+
+def comet_kv4_attention(cache, batch, Q, out, heads: int, q_stride: int, out_stride: int,
+                        scale: float, window: int = 0, workspace=None, workspace_bytes=None,
+                        stream=None) -> None:
+    if cache is not None and batch is not None:
+        c, b = getattr(cache, "struct", cache), getattr(batch, "struct", batch)
+        if b.M > 0 and heads > 0:
+            _row_room(Q, b.M, q_stride, heads * c.head_dim, "Q")
+            _row_room(out, b.M, out_stride, heads * c.head_dim, "out")
+    have = _nbytes(workspace)
+    if workspace_bytes is None:
+        workspace_bytes = have or 0
+    elif have is not None and have < workspace_bytes:
+        raise ValueError(f"workspace: {have} bytes, workspace_bytes says {workspace_bytes}")
+    _check(lib().comet_kv4_attention(_struct(cache), _struct(batch), _ptr(Q), _ptr(out), heads,
+                                     q_stride, out_stride, scale, window, _ptr(workspace),
+                                     workspace_bytes, _stream(stream)))
+
+
+def comet_kv4_attention_workspace(cache, batch, heads: int, num_cus: int) -> int:
+    return int(lib().comet_kv4_attention_workspace(_struct(cache), _struct(batch), heads, num_cus))
+
+
 def comet_w4ax_gemm_swiglu_quant(A_packed, group_prec_map, a_scales, W_packed, w_scales, M: int,
                                  N: int, K: int, G: int, out_prec_map, out_A_packed, out_a_scales,
                                  stream=None) -> None:
@@ -478,6 +587,249 @@ def kv4_dequantize(codes, params, G: int = 128, stream=None):
     _exact(params, T * (C // G) * 2, "params")
     out = torch.empty((T, C), dtype=torch.float16, device=codes.device)
     comet_kv4_dequantize(codes, params, out, T, C, G, stream)
+    return out
+
+
+def rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "none",
+                     factor: float = 1.0, low: float = 1.0, high: float = 4.0,
+                     original_len: float = 8192.0):
+    """Host: (float64 numpy array [rot_dim / 2] of radians per position, mscale) for
+    ``rope``; scaling is a key of ROPE_SCALINGS (comet_rope_scaling_t)."""
+    if scaling not in ROPE_SCALINGS:
+        raise ValueError(f"scaling: {scaling!r}, known are {', '.join(ROPE_SCALINGS)}")
+    freqs = np.empty(max(rot_dim // 2, 1), np.float64)
+    mscale = np.ones(1, np.float32)
+    comet_rope_frequencies(freqs, rot_dim, base, ROPE_SCALINGS[scaling], factor, low, high,
+                           original_len, mscale)
+    return freqs, float(mscale[0])
+
+
+def _heads_of(t, name: str):
+    """(rows, heads, channels, row stride) of a float16 tensor [rows][heads][channels]
+    on the current device whose heads are contiguous; the rows may lie in a wider
+    buffer (the q, k or v columns of a qkv output)."""
+    import torch
+
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != torch.float16 or t.dim() != 3:
+        got = (f"{t.dtype} {tuple(t.shape)} on {t.device}" if isinstance(t, torch.Tensor)
+               else type(t).__name__)
+        raise ValueError(f"{name}: need a float16 CUDA tensor [rows][heads][channels], got {got}")
+    M, H, D = t.shape
+    s0, s1, s2 = t.stride()
+    if (D > 1 and s2 != 1) or (H > 1 and s1 != D) or (M > 1 and s0 < H * D):
+        raise ValueError(f"{name}: heads and channels must be contiguous and rows apart, got "
+                         f"strides {t.stride()} for {tuple(t.shape)}")
+    if M == 1:
+        s0 = H * D  # of no meaning then
+    return M, H, D, s0
+
+
+def _on_current(*named) -> None:
+    """The tensors are on the device that the call will run on."""
+    import torch
+
+    at = torch.cuda.current_device()
+    for name, index in named:
+        if index != at:
+            raise ValueError(f"{name}: on device {index}, the current device is {at}")
+
+
+def _new(shape, dtype, device, stream):
+    """Memory for work on `stream`: it is taken from that stream's own pool, so that no
+    other stream's work is still using it, or gets it before this work is done."""
+    import torch
+
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    s = torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream
+    with torch.cuda.stream(s):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def rope(x, positions, freqs, interleaved: bool = False, mscale: float = 1.0, out=None,
+         stream=None):
+    """Rotary positions.  x: float16 CUDA tensor [M][heads][head_dim] (rows may lie in a
+    wider buffer); positions: int32 [M]; freqs: float64 [rot_dim / 2], of
+    ``rope_frequencies``, on the GPU.  Returns out (out=x rotates in place)."""
+    import torch
+
+    M, H, D, xs = _heads_of(x, "x")
+    _tensor(positions, "int32", "positions")
+    _tensor(freqs, "float64", "freqs")
+    _exact(positions, M, "positions")
+    if out is None:
+        out = _new((M, H, D), torch.float16, x.device, stream)
+    oM, oH, oD, os_ = _heads_of(out, "out")
+    if (oM, oH, oD) != (M, H, D):
+        raise ValueError(f"out: shape {tuple(out.shape)}, expected {(M, H, D)}")
+    _on_current(("x", x.get_device()), ("positions", positions.get_device()),
+                ("freqs", freqs.get_device()), ("out", out.get_device()))
+    _check(lib().comet_rope(x.data_ptr(), positions.data_ptr(), freqs.data_ptr(), out.data_ptr(),
+                            M, H, D, 2 * freqs.numel(), xs, os_, int(bool(interleaved)), mscale,
+                            _stream(stream)))
+    return out
+
+
+class KV4Cache:
+    """A paged 4-bit K/V cache: codes uint8 [num_pages][kv_heads][page_size][head_dim / 2]
+    and params float16 [num_pages][kv_heads][page_size][head_dim / G][2] of K and of V,
+    contiguous CUDA tensors that this object keeps alive."""
+
+    def __init__(self, k_codes, k_params, v_codes, v_params):
+        for name, t, dtype, dim in (("k_codes", k_codes, "uint8", 4),
+                                    ("k_params", k_params, "float16", 5),
+                                    ("v_codes", v_codes, "uint8", 4),
+                                    ("v_params", v_params, "float16", 5)):
+            _tensor(t, dtype, name)
+            if t.dim() != dim:
+                raise ValueError(f"{name}: {t.dim()} dimensions, expected {dim}")
+        pages, heads, size, half = k_codes.shape
+        groups = k_params.shape[3]
+        want = {"k_params": (pages, heads, size, groups, 2), "v_codes": (pages, heads, size, half),
+                "v_params": (pages, heads, size, groups, 2)}
+        for name, t in (("k_params", k_params), ("v_codes", v_codes), ("v_params", v_params)):
+            if tuple(t.shape) != want[name]:
+                raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {want[name]}")
+            if t.device != k_codes.device:
+                raise ValueError(f"{name}: on {t.device}, k_codes on {k_codes.device}")
+        if groups < 1 or (2 * half) % groups:
+            raise ValueError(f"k_params: {groups} groups do not divide {2 * half} channels")
+        self.k_codes, self.k_params = k_codes, k_params
+        self.v_codes, self.v_params = v_codes, v_params
+        self.num_pages, self.page_size, self.kv_heads = pages, size, heads
+        self.head_dim, self.G = 2 * half, 2 * half // groups
+        self.device = k_codes.device
+        self.struct = KV4CacheStruct(k_codes.data_ptr(), k_params.data_ptr(), v_codes.data_ptr(),
+                                     v_params.data_ptr(), pages, size, heads, self.head_dim,
+                                     self.G)
+
+    @classmethod
+    def empty(cls, num_pages: int, page_size: int, kv_heads: int, head_dim: int, G: int = 128,
+              device="cuda"):
+        """A new cache (its contents are written before they are read)."""
+        import torch
+
+        if G < 1 or head_dim % G:
+            raise ValueError(f"head_dim={head_dim} is not a multiple of G={G}")
+        rows = (num_pages, kv_heads, page_size)
+        codes = [torch.empty(rows + (head_dim // 2,), dtype=torch.uint8, device=device)
+                 for _ in "kv"]
+        params = [torch.empty(rows + (head_dim // G, 2), dtype=torch.float16, device=device)
+                  for _ in "kv"]
+        return cls(codes[0], params[0], codes[1], params[1])
+
+
+class KV4Batch:
+    """The rows of a call and where their sequences lie: row_start int32 [B + 1], seq_lens
+    int32 [B], block_table int32 [B][max_pages] (comet_kv4_batch_t), CUDA tensors that this
+    object keeps alive; their contents are read when the work runs.  M: rows of the buffers;
+    max_rows: the most rows of one sequence (M if not given)."""
+
+    def __init__(self, row_start, seq_lens, block_table, M: int, max_rows: Optional[int] = None):
+        for name, t in (("row_start", row_start), ("seq_lens", seq_lens),
+                        ("block_table", block_table)):
+            _tensor(t, "int32", name)
+            if t.device != seq_lens.device:
+                raise ValueError(f"{name}: on {t.device}, seq_lens on {seq_lens.device}")
+        B = seq_lens.numel()
+        _exact(row_start, B + 1, "row_start")
+        if block_table.dim() != 2 or block_table.shape[0] != B:
+            raise ValueError(f"block_table: shape {tuple(block_table.shape)}, expected ({B}, pages)")
+        self.row_start, self.seq_lens, self.block_table = row_start, seq_lens, block_table
+        self.B, self.M, self.max_pages = B, M, block_table.shape[1]
+        self.max_rows = M if max_rows is None else max_rows
+        self.device = seq_lens.device
+        self.struct = KV4BatchStruct(row_start.data_ptr(), seq_lens.data_ptr(),
+                                     block_table.data_ptr(), B, M, self.max_pages, self.max_rows)
+
+
+def _kv4_rows(t, cache, batch, name: str):
+    """Row stride of a K or V buffer of this cache and batch."""
+    M, H, D, stride = _heads_of(t, name)
+    if (M, H, D) != (batch.M, cache.kv_heads, cache.head_dim):
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected "
+                         f"{(batch.M, cache.kv_heads, cache.head_dim)}")
+    return stride
+
+
+def kv4_append(cache: KV4Cache, batch: KV4Batch, k, v, stream=None) -> None:
+    """Quantizes the rows k, v (float16 [M][kv_heads][head_dim], rows may lie in a wider
+    buffer) into the cache, each to its sequence's last positions."""
+    ks, vs = _kv4_rows(k, cache, batch, "k"), _kv4_rows(v, cache, batch, "v")
+    _on_current(("cache", cache.device.index), ("batch", batch.device.index),
+                ("k", k.get_device()), ("v", v.get_device()))
+    _check(lib().comet_kv4_append(ctypes.addressof(cache.struct), ctypes.addressof(batch.struct),
+                                  k.data_ptr(), v.data_ptr(), ks, vs, _stream(stream)))
+
+
+def kv4_gather(cache: KV4Cache, batch: KV4Batch, k_out=None, v_out=None, stream=None):
+    """Reads the last rows of each sequence back: (k, v) float16 [M][kv_heads][head_dim].
+    Rows in no sequence are left as they are (uninitialized in a new tensor)."""
+    import torch
+
+    shape = (batch.M, cache.kv_heads, cache.head_dim)
+    k, v = (_new(shape, torch.float16, cache.device, stream) if t is None else t
+            for t in (k_out, v_out))
+    ks, vs = _kv4_rows(k, cache, batch, "k_out"), _kv4_rows(v, cache, batch, "v_out")
+    _on_current(("cache", cache.device.index), ("batch", batch.device.index),
+                ("k_out", k.get_device()), ("v_out", v.get_device()))
+    _check(lib().comet_kv4_gather(ctypes.addressof(cache.struct), ctypes.addressof(batch.struct),
+                                  k.data_ptr(), v.data_ptr(), ks, vs, _stream(stream)))
+    return k, v
+
+
+_cus = {}
+
+
+def _num_cus(device) -> int:
+    n = _cus.get(device.index)
+    if n is None:
+        import torch
+
+        n = _cus[device.index] = torch.cuda.get_device_properties(device).multi_processor_count
+    return n
+
+
+def kv4_attention_workspace(q, cache: KV4Cache, batch: KV4Batch, stream=None):
+    """A workspace tensor for kv4_attention calls of these sizes that do not overlap (None
+    where none is needed)."""
+    import torch
+
+    n = lib().comet_kv4_attention_workspace(ctypes.addressof(cache.struct),
+                                            ctypes.addressof(batch.struct), q.shape[1],
+                                            _num_cus(cache.device))
+    return _new(n, torch.uint8, cache.device, stream) if n else None
+
+
+def kv4_attention(q, cache: KV4Cache, batch: KV4Batch, scale: Optional[float] = None,
+                  window: int = 0, out=None, workspace=None, stream=None):
+    """Causal attention of the batch's rows q (float16 [M][heads][head_dim], rows may lie in
+    a wider buffer) over the cache, which holds their own tokens already.  scale defaults to
+    head_dim ** -0.5; workspace (of ``kv4_attention_workspace``) is allocated when not given.
+    Returns out; rows in no sequence are left as they are (uninitialized in a new tensor)."""
+    import torch
+
+    M, H, D, qs = _heads_of(q, "q")
+    if (M, D) != (batch.M, cache.head_dim):
+        raise ValueError(f"q: shape {tuple(q.shape)}, expected "
+                         f"({batch.M}, heads, {cache.head_dim})")
+    if out is None:
+        out = _new((M, H, D), torch.float16, q.device, stream)
+    oM, oH, oD, os_ = _heads_of(out, "out")
+    if (oM, oH, oD) != (M, H, D):
+        raise ValueError(f"out: shape {tuple(out.shape)}, expected {(M, H, D)}")
+    if workspace is None:
+        workspace = kv4_attention_workspace(q, cache, batch, stream)
+    else:
+        _tensor(workspace, "uint8", "workspace")
+        _on_current(("workspace", workspace.get_device()))
+    _on_current(("q", q.get_device()), ("cache", cache.device.index),
+                ("batch", batch.device.index), ("out", out.get_device()))
+    _check(lib().comet_kv4_attention(
+        ctypes.addressof(cache.struct), ctypes.addressof(batch.struct), q.data_ptr(),
+        out.data_ptr(), H, qs, os_, D ** -0.5 if scale is None else scale, window,
+        None if workspace is None else workspace.data_ptr(),
+        0 if workspace is None else workspace.numel(), _stream(stream)))
     return out
 
 

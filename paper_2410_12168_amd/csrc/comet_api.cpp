@@ -7,6 +7,7 @@
 #include <cstdio>
 #include <cstdlib>
 #include <algorithm>
+#include <cmath>
 #include <cstring>
 #include <map>
 #include <mutex>
@@ -17,6 +18,7 @@
 #include "../../include/comet.h"
 #include "kernels.h"
 #include "scheduler.h"
+#include "serving.h"
 
 #ifndef COMET_SOURCE_STAMP
 #define COMET_SOURCE_STAMP "unstamped"
@@ -575,6 +577,76 @@ comet_status_t run_gemm_noalloc(const uint8_t* A, const uint8_t* prec, const uin
                   "gemm launch");
 }
 
+// The static fields of a paged cache; the sizes only where `buffers` is false.
+comet_status_t check_cache(const comet_kv4_cache_t* c, bool buffers, comet::PagedCache* out) {
+  if (!c) return fail(COMET_ERR_INVALID_ARG, "cache is null");
+  if (c->head_dim != 64 && c->head_dim != 128)
+    return fail(COMET_ERR_UNSUPPORTED, "head_dim=%d: 64 or 128 channels", c->head_dim);
+  if ((c->G != 32 && c->G != 64 && c->G != 128) || c->G > c->head_dim)
+    return fail(COMET_ERR_UNSUPPORTED, "G=%d: groups of 32, 64 or 128 channels within head_dim=%d",
+                c->G, c->head_dim);
+  if (c->page_size < 16 || c->page_size > 1024 || (c->page_size & (c->page_size - 1)))
+    return fail(COMET_ERR_UNSUPPORTED, "page_size=%d: a power of two, 16 .. 1024", c->page_size);
+  if (c->num_pages < 1 || c->kv_heads < 1)
+    return fail(COMET_ERR_INVALID_ARG, "num_pages=%d, kv_heads=%d must be >= 1", c->num_pages,
+                c->kv_heads);
+  if (c->kv_heads > 1024)
+    return fail(COMET_ERR_UNSUPPORTED, "kv_heads=%d exceeds 1024", c->kv_heads);
+  if (buffers) {
+    if (!c->k_codes || !c->k_params || !c->v_codes || !c->v_params)
+      return fail(COMET_ERR_INVALID_ARG, "null pointer in the cache");
+    if (!aligned16(c->k_codes) || !aligned16(c->k_params) || !aligned16(c->v_codes) ||
+        !aligned16(c->v_params))
+      return fail(COMET_ERR_INVALID_ARG, "cache buffers must be 16-byte aligned");
+  }
+  *out = {c->k_codes, c->k_params, c->v_codes, c->v_params, c->num_pages,
+          __builtin_ctz((unsigned)c->page_size), c->kv_heads, c->head_dim, c->G};
+  return COMET_OK;
+}
+
+comet_status_t check_batch(const comet_kv4_batch_t* b, const comet::PagedCache& c, bool buffers,
+                           comet::PagedBatch* out) {
+  if (!b) return fail(COMET_ERR_INVALID_ARG, "batch is null");
+  if (b->B < 1 || b->M < 1 || b->max_pages < 1 || b->max_rows < 1)
+    return fail(COMET_ERR_INVALID_ARG, "B=%d, M=%d, max_pages=%d, max_rows=%d must be >= 1", b->B,
+                b->M, b->max_pages, b->max_rows);
+  if (b->B > 65536) return fail(COMET_ERR_UNSUPPORTED, "B=%d exceeds 65536", b->B);
+  if (b->M > kMaxQuantRows)
+    return fail(COMET_ERR_UNSUPPORTED, "M=%d exceeds %d rows per call", b->M, kMaxQuantRows);
+  if (b->max_pages > (1 << 30) >> c.page_shift)
+    return fail(COMET_ERR_UNSUPPORTED, "max_pages=%d pages of %d tokens exceed 2^30", b->max_pages,
+                1 << c.page_shift);
+  if (buffers) {
+    if (!b->row_start || !b->seq_lens || !b->block_table)
+      return fail(COMET_ERR_INVALID_ARG, "null pointer in the batch");
+    const uintptr_t a = reinterpret_cast<uintptr_t>(b->row_start) |
+                        reinterpret_cast<uintptr_t>(b->seq_lens) |
+                        reinterpret_cast<uintptr_t>(b->block_table);
+    if (a & 3u) return fail(COMET_ERR_INVALID_ARG, "batch arrays must be 4-byte aligned");
+  }
+  *out = {b->row_start, b->seq_lens, b->block_table, b->B, b->M, b->max_pages,
+          std::min(b->max_rows, b->M)};
+  return COMET_OK;
+}
+
+// Rows of `heads` heads, `stride` channels apart.
+comet_status_t check_rows(const void* p, int stride, int heads, int head_dim, const char* name) {
+  if (!p) return fail(COMET_ERR_INVALID_ARG, "%s is null", name);
+  if (!aligned16(p)) return fail(COMET_ERR_INVALID_ARG, "%s must be 16-byte aligned", name);
+  if (stride % 8 || stride < heads * head_dim)
+    return fail(COMET_ERR_INVALID_ARG, "%s: stride %d must be a multiple of 8 and at least %d",
+                name, stride, heads * head_dim);
+  return COMET_OK;
+}
+
+comet_status_t check_heads(int heads, int kv_heads) {
+  if (heads < 1 || heads % kv_heads)
+    return fail(COMET_ERR_INVALID_ARG, "heads=%d must be a positive multiple of kv_heads=%d", heads,
+                kv_heads);
+  if (heads > 1024) return fail(COMET_ERR_UNSUPPORTED, "heads=%d exceeds 1024", heads);
+  return COMET_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -713,6 +785,126 @@ comet_status_t comet_kv4_dequantize(const uint8_t* codes, const uint16_t* params
   if ((st = current_device(&dev, &info))) return st;
   return launched(comet::launch_kv4_dequantize(codes, params, out, T, C, G, stream),
                   "kv4_dequantize launch");
+}
+
+comet_status_t comet_rope(const uint16_t* X, const int32_t* positions, const double* freqs,
+                          uint16_t* out, int M, int heads, int head_dim, int rot_dim, int x_stride,
+                          int out_stride, int interleaved, float mscale, hipStream_t stream) {
+  if (!X || !positions || !freqs || !out) return fail(COMET_ERR_INVALID_ARG, "null pointer");
+  if (M < 1 || heads < 1) return fail(COMET_ERR_INVALID_ARG, "M=%d, heads=%d must be >= 1", M, heads);
+  if (M > kMaxQuantRows || heads > 65535)
+    return fail(COMET_ERR_UNSUPPORTED, "M=%d, heads=%d exceed %d rows or 65535 heads", M, heads,
+                kMaxQuantRows);
+  if (rot_dim < 2 || rot_dim % 2 || rot_dim > head_dim)
+    return fail(COMET_ERR_INVALID_ARG, "rot_dim=%d must be even, 2 .. head_dim=%d", rot_dim,
+                head_dim);
+  if (head_dim > 1024) return fail(COMET_ERR_UNSUPPORTED, "head_dim=%d exceeds 1024", head_dim);
+  if (x_stride < heads * head_dim || out_stride < heads * head_dim)
+    return fail(COMET_ERR_INVALID_ARG, "strides %d, %d must be at least heads * head_dim = %d",
+                x_stride, out_stride, heads * head_dim);
+  if (X == out && x_stride != out_stride)
+    return fail(COMET_ERR_INVALID_ARG, "in place, out_stride=%d must equal x_stride=%d", out_stride,
+                x_stride);
+  if (!std::isfinite(mscale)) return fail(COMET_ERR_INVALID_ARG, "mscale is not finite");
+  if (((reinterpret_cast<uintptr_t>(X) | reinterpret_cast<uintptr_t>(out)) & 1u) ||
+      (reinterpret_cast<uintptr_t>(positions) & 3u) || (reinterpret_cast<uintptr_t>(freqs) & 7u))
+    return fail(COMET_ERR_INVALID_ARG, "X and out must be 2-byte, positions 4-byte and freqs "
+                "8-byte aligned");
+  comet_status_t st;
+  int dev;
+  DeviceInfo info;
+  if ((st = current_device(&dev, &info))) return st;
+  const comet::RopeArgs a{X, positions, freqs, out, M, heads, head_dim, rot_dim, x_stride,
+                          out_stride, interleaved != 0, mscale, info.cus};
+  return launched(comet::launch_rope(a, stream), "rope launch");
+}
+
+comet_status_t comet_rope_frequencies(double* freqs, int rot_dim, double base, int scaling,
+                                      double factor, double low, double high, double original_len,
+                                      float* mscale) {
+  if (!freqs) return fail(COMET_ERR_INVALID_ARG, "null pointer");
+  const char* why = comet::rope_frequencies(freqs, rot_dim, base, scaling, factor, low, high,
+                                            original_len, mscale);
+  if (why) return fail(COMET_ERR_INVALID_ARG, "%s", why);
+  return ok();
+}
+
+comet_status_t comet_kv4_append(const comet_kv4_cache_t* cache, const comet_kv4_batch_t* batch,
+                                const uint16_t* K, const uint16_t* V, int k_stride, int v_stride,
+                                hipStream_t stream) {
+  comet::PagedCache c;
+  comet::PagedBatch b;
+  comet_status_t st;
+  if ((st = check_cache(cache, true, &c))) return st;
+  if ((st = check_batch(batch, c, true, &b))) return st;
+  if ((st = check_rows(K, k_stride, c.kv_heads, c.head_dim, "K"))) return st;
+  if ((st = check_rows(V, v_stride, c.kv_heads, c.head_dim, "V"))) return st;
+  int dev;
+  DeviceInfo info;
+  if ((st = current_device(&dev, &info))) return st;
+  const comet::RowBuffers r{K, V, nullptr, nullptr, k_stride, v_stride};
+  return launched(comet::launch_kv4_append(c, b, r, info.cus, stream), "kv4_append launch");
+}
+
+comet_status_t comet_kv4_gather(const comet_kv4_cache_t* cache, const comet_kv4_batch_t* batch,
+                                uint16_t* K, uint16_t* V, int k_stride, int v_stride,
+                                hipStream_t stream) {
+  comet::PagedCache c;
+  comet::PagedBatch b;
+  comet_status_t st;
+  if ((st = check_cache(cache, true, &c))) return st;
+  if ((st = check_batch(batch, c, true, &b))) return st;
+  if (!K && !V) return fail(COMET_ERR_INVALID_ARG, "K and V are both null");
+  if (K && (st = check_rows(K, k_stride, c.kv_heads, c.head_dim, "K"))) return st;
+  if (V && (st = check_rows(V, v_stride, c.kv_heads, c.head_dim, "V"))) return st;
+  int dev;
+  DeviceInfo info;
+  if ((st = current_device(&dev, &info))) return st;
+  const comet::RowBuffers r{nullptr, nullptr, K, V, k_stride, v_stride};
+  return launched(comet::launch_kv4_gather(c, b, r, info.cus, stream), "kv4_gather launch");
+}
+
+size_t comet_kv4_attention_workspace(const comet_kv4_cache_t* cache,
+                                     const comet_kv4_batch_t* batch, int heads, int num_cus) {
+  comet::PagedCache c;
+  comet::PagedBatch b;
+  if (check_cache(cache, false, &c) || check_batch(batch, c, false, &b) ||
+      check_heads(heads, c.kv_heads))
+    return 0;
+  if (num_cus < 1) {
+    fail(COMET_ERR_INVALID_ARG, "num_cus=%d must be >= 1", num_cus);
+    return 0;
+  }
+  ok();
+  return comet::attention_workspace(c, b, heads, num_cus);
+}
+
+comet_status_t comet_kv4_attention(const comet_kv4_cache_t* cache, const comet_kv4_batch_t* batch,
+                                   const uint16_t* Q, uint16_t* out, int heads, int q_stride,
+                                   int out_stride, float scale, int window, void* workspace,
+                                   size_t workspace_bytes, hipStream_t stream) {
+  comet::PagedCache c;
+  comet::PagedBatch b;
+  comet_status_t st;
+  if ((st = check_cache(cache, true, &c))) return st;
+  if ((st = check_batch(batch, c, true, &b))) return st;
+  if ((st = check_heads(heads, c.kv_heads))) return st;
+  if ((st = check_rows(Q, q_stride, heads, c.head_dim, "Q"))) return st;
+  if ((st = check_rows(out, out_stride, heads, c.head_dim, "out"))) return st;
+  if (!std::isfinite(scale)) return fail(COMET_ERR_INVALID_ARG, "scale is not finite");
+  if (window < 0) return fail(COMET_ERR_INVALID_ARG, "window=%d must be >= 0", window);
+  if (!aligned16(workspace))
+    return fail(COMET_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
+  int dev;
+  DeviceInfo info;
+  if ((st = current_device(&dev, &info))) return st;
+  const size_t need = comet::attention_workspace(c, b, heads, info.cus);
+  if (need && (!workspace || workspace_bytes < need))
+    return fail(COMET_ERR_INVALID_ARG, "workspace of %zu bytes, the call needs %zu",
+                workspace ? workspace_bytes : 0, need);
+  const comet::AttentionArgs a{Q, out, heads, q_stride, out_stride, scale, window, workspace,
+                               info.cus};
+  return launched(comet::launch_kv4_attention(c, b, a, stream), "kv4_attention launch");
 }
 
 comet_status_t comet_w4ax_gemm(const uint8_t* A_packed, const uint8_t* prec,
