@@ -875,6 +875,10 @@ size_t comet_kv4_attention_workspace(const comet_kv4_cache_t* cache,
     fail(COMET_ERR_INVALID_ARG, "num_cus=%d must be >= 1", num_cus);
     return 0;
   }
+  if (const char* why = comet::attention_refusal(c, b, heads, num_cus)) {
+    fail(COMET_ERR_UNSUPPORTED, "M=%d, B=%d, heads=%d: %s", b.M, b.B, heads, why);
+    return 0;
+  }
   ok();
   return comet::attention_workspace(c, b, heads, num_cus);
 }
@@ -898,6 +902,8 @@ comet_status_t comet_kv4_attention(const comet_kv4_cache_t* cache, const comet_k
   int dev;
   DeviceInfo info;
   if ((st = current_device(&dev, &info))) return st;
+  if (const char* why = comet::attention_refusal(c, b, heads, info.cus))
+    return fail(COMET_ERR_UNSUPPORTED, "M=%d, B=%d, heads=%d: %s", b.M, b.B, heads, why);
   const size_t need = comet::attention_workspace(c, b, heads, info.cus);
   if (need && (!workspace || workspace_bytes < need))
     return fail(COMET_ERR_INVALID_ARG, "workspace of %zu bytes, the call needs %zu",

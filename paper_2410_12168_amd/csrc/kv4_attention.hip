@@ -2,18 +2,43 @@
 // gfx950.
 //
 // Row i of sequence b, q head h, at position p = L_b - n_b + i:
-//   x_j = scale * q . k_j,  out = sum_j exp(x_j) v_j / sum_j exp(x_j)
+//   x_j = scale * q . k_j,  out = sum_j w_j v_j / sum_j w_j,  w_j = exp(x_j)
 // over the tokens j <= p that the row sees, with the cached value q s + mn of a
-// code.  A group's scale and offset are taken out of the sums:
+// code.  A group's scale and offset are taken out of the sums,
 //   q . k_j = sum_g s_jg (q . codes_j)_g + mn_jg (sum q)_g
-//   sum_j w_j v_j = sum_j (w_j s_j) codes_j + sum_j w_j mn_j
-// One pass over the tokens with the running maximum and sum of the softmax.
+//   sum_j w_j v_j = sum_j (w_j s_j) codes_j + sum_j w_j mn_j,
+// so that both products run on the codes themselves.  One pass over the tokens
+// with the running maximum and sum of the softmax.
 //
-// Work decomposition: one wave per row and head, 64 tokens at a time: a lane per
-// token for the scores, a lane per channel pair for the weighted sum.
+// Matrix operands (v_mfma_f32_16x16x32_f16; rows: tokens or channels, columns:
+// 16 rows of q):
+//   - a code c is the fp16 subnormal c * 2^-24, which the matrix cores keep:
+//     two masks and a shift make eight of them from a dword, every second one
+//     16 times larger (its nibble sits four bits higher), which the other
+//     operand takes back.  The order within a dword is (0, 4, 1, 5, 2, 6, 3, 7).
+//   - q is scaled by a power of two per row (largest value in [2^10, 2^11)), so
+//     that neither that factor nor subnormals cost bits.
+//   - w_j s_j is scaled by a power of two per wave, so that the largest scale of
+//     the tokens so far lands in [2^14, 2^15): a weight loses bits only where it
+//     is 2^-28 of the largest.  It is rounded to fp16 (2^-11 relative).
+//   - V's operand needs 8 tokens of a channel in a lane; the cache has channels
+//     in a row.  The transposing LDS read (ds_read_b64_tr_b4: 16 rows of 16
+//     nibbles) turns 16 tokens x 16 channels at a time.
+//   - token 16 h + 4 j + r of a 64-token tile is row 4 h + r of the j-th score
+//     product, so a lane's scores are those of the tokens that its lanes of V's
+//     operand hold: the weights go from one product into the other in place.
+//
+// Work decomposition: a block of four waves takes one (sequence, kv head, 16 C
+// rows of its q heads, range of tokens); the waves take turns at its 64-token
+// tiles and add up in LDS at the end.  The token ranges follow from the lengths
+// on the device (find_unit): every block of every sequence gets about the same
+// number of tiles, about `target` ranges in all, and a second kernel adds up the
+// ranges of a sequence that has more than one.
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+
+#include <algorithm>
 
 #include "paged.h"
 
@@ -21,105 +46,714 @@ namespace comet {
 
 namespace {
 
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
 constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kNone = -1e30f;  // maximum of no scores
+constexpr int kTile = 64;        // tokens a wave takes at a time
+constexpr int kWaves = 4;
+// fewest tiles in a range: one for each wave
+constexpr int kMinTiles = kWaves;
 
 __device__ inline float low_half(uint32_t w) {
   return __half2float(__ushort_as_half((unsigned short)w));
 }
 
-__device__ inline float wave_max(float v) {
-  #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) v = fmaxf(v, __shfl_xor(v, o));
-  return v;
+// Sum and maximum over the four lanes of a column (l, l ^ 16, l ^ 32, l ^ 48).
+__device__ inline float quad_max(float v) {
+  v = fmaxf(v, __shfl_xor(v, 16));
+  return fmaxf(v, __shfl_xor(v, 32));
+}
+__device__ inline float quad_sum(float v) {
+  v += __shfl_xor(v, 16);
+  return v + __shfl_xor(v, 32);
 }
 
-__device__ inline float wave_sum(float v) {
+// a * b, and 0 where either is 0 whatever the other is (v_mul_legacy_f32).
+extern "C" __device__ float mul_zero(float a, float b) __asm("llvm.amdgcn.fmul.legacy");
+
+// Eight codes as fp16, order (0, 4, 1, 5, 2, 6, 3, 7), times 2^-24 and, for the
+// odd ones, 2^-20.
+__device__ inline f16x8 codes_f16(uint32_t x) {
+  const u32x4 r = {x & 0x000F000Fu, x & 0x00F000F0u, (x >> 8) & 0x000F000Fu,
+                   (x >> 8) & 0x00F000F0u};
+  return __builtin_bit_cast(f16x8, r);
+}
+
+// ---- which part of the work ------------------------------------------------
+
+struct UnitShape {
+  int group;     // q heads per kv head
+  int rows;      // q rows (of all heads of a group) per block
+  int window;
+  int target;    // token ranges to aim at, per kv head
+};
+
+struct SeqWork {
+  int start, n;        // first row, rows
+  long long len;       // tokens
+  long long blocks;    // row blocks
+  long long first;     // first tile that any row sees
+  long long tiles;     // tiles from there on (1 at least)
+};
+
+__device__ inline SeqWork seq_work(const PagedBatch& b, int page_shift, const UnitShape& u,
+                                   int seq) {
+  SeqWork w{0, 0, 0, 0, 0, 0};
+  if (seq >= b.B) return w;
+  w.start = max(0, min(b.M, b.row_start[seq]));
+  w.n = max(0, max(0, min(b.M, b.row_start[seq + 1])) - w.start);
+  w.len = b.seq_lens[seq];
+  const long long cap = (long long)b.max_pages << page_shift;
+  const long long seen = max(0ll, min(w.len, cap));
+  const long long low = u.window > 0 ? max(0ll, w.len - w.n - u.window + 1) : 0ll;
+  w.blocks = ((long long)w.n * u.group + u.rows - 1) / u.rows;
+  w.first = low / kTile;
+  w.tiles = max(1ll, (seen + kTile - 1) / kTile - w.first);
+  return w;
+}
+
+// One block's work: row block `block` of sequence `seq`, range `range` of `ranges`
+// with `per` tiles each.
+struct Unit {
+  int seq, block, range, ranges;
+  long long per;
+  uint32_t before;   // units of earlier sequences
+  uint32_t slot;     // partial results of earlier sequences
+  SeqWork w;
+};
+
+// Lane `at`'s value (`at` the same in all lanes) where the compiler knows that all
+// lanes have it.
+__device__ inline int from_lane(int v, int at) { return __builtin_amdgcn_readlane(v, at); }
+__device__ inline long long from_lane(long long v, int at) {
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, at);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), at);
+  return (long long)((unsigned long long)hi << 32 | lo);
+}
+
+template <typename T>
+__device__ inline T wave_sum(T v) {
   #pragma unroll
   for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
   return v;
 }
 
-__global__ __launch_bounds__(64) void kv4_attention_row_kernel(PagedCache c, PagedBatch b,
-                                                               AttentionArgs a) {
-  __shared__ float q[128];
-  __shared__ float weight[64];
-  __shared__ int pages[64];
-  const int lane = threadIdx.x, h = blockIdx.y;
+// Tiles of a range, from the work of all sequences: the same in every wave of a
+// launch.
+__device__ inline long long tiles_per_range(const PagedBatch& b, int page_shift,
+                                            const UnitShape& u) {
+  const int lane = threadIdx.x & 63;
+  double total = 0.0;  // whole numbers, exact
+  for (int s = 0; s < b.B; s += 64) {
+    const SeqWork w = seq_work(b, page_shift, u, s + lane);
+    total += (double)w.blocks * (double)w.tiles;
+  }
+  return from_lane(max((long long)kMinTiles, (long long)ceil(wave_sum(total) / u.target)), 0);
+}
+
+// Unit `index` (counted over sequences, row blocks and ranges), or the units
+// before sequence `want` (want >= 0).  False if there is none.  Both counts, of
+// all units and of those that leave partial results, run in one sum of 32 + 32
+// bits.
+__device__ inline bool find_unit(const PagedBatch& b, int page_shift, const UnitShape& u,
+                                 uint32_t index, int want, Unit* out) {
+  const int lane = threadIdx.x & 63;
+  const long long per = tiles_per_range(b, page_shift, u);
+  long long before = 0;
+  for (int s = 0; s < b.B; s += 64) {
+    const SeqWork w = seq_work(b, page_shift, u, s + lane);
+    const long long ranges = (w.tiles + per - 1) / per;
+    long long mine = w.blocks * ranges;
+    if (ranges > 1) mine |= mine << 32;
+    long long upto = mine;
+    #pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const long long v = __shfl_up(upto, o);
+      if (lane >= o) upto += v;
+    }
+    const bool here = want >= 0 ? s + lane == want : (uint32_t)(before + upto) > index;
+    const unsigned long long hit = __ballot(here);
+    if (hit) {
+      const int at = __builtin_amdgcn_readfirstlane(__ffsll((long long)hit) - 1);
+      const long long sum = before + from_lane(upto - mine, at);
+      out->seq = s + at;
+      out->per = per;
+      out->before = (uint32_t)sum;
+      out->slot = (uint32_t)(sum >> 32);
+      out->ranges = (int)from_lane(ranges, at);
+      out->w.start = from_lane(w.start, at);
+      out->w.n = from_lane(w.n, at);
+      out->w.len = from_lane(w.len, at);
+      out->w.blocks = from_lane(w.blocks, at);
+      out->w.first = from_lane(w.first, at);
+      out->w.tiles = from_lane(w.tiles, at);
+      if (want < 0) {
+        const uint32_t k = index - out->before;
+        // the last row blocks see the most tokens: they come first
+        out->block = (int)(out->w.blocks - 1 - k / (uint32_t)out->ranges);
+        out->range = (int)(k % (uint32_t)out->ranges);
+        out->slot += k;
+      }
+      return true;
+    }
+    before += from_lane(upto, 63);
+  }
+  return false;
+}
+
+// Partial results in the workspace: [slot][kv head][rows][D] sums and
+// [slot][kv head][rows][2] {maximum (log2), sum of weights}.  A sequence with more
+// than one range has more than `per` tiles, and `per` is at least all tiles over
+// `target`: there are fewer than 2 * target slots.
+struct Partials {
+  float* sums;
+  float* stats;
+  uint32_t slots;
+};
+
+// ---- the products --------------------------------------------------------------
+
+template <int D, int G, int C>
+__global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_kernel(
+    PagedCache c, PagedBatch b, AttentionArgs a, UnitShape u, Partials part) {
+  constexpr int NG = D / G;         // groups of a head
+  constexpr int KS = D / 32;        // steps of the score product
+  constexpr int DB = D / 16;        // 16-channel blocks of the output
+  constexpr int ROW = D / 2;        // bytes of a row of codes
+  constexpr int VL = ROW / 16;      // 16-byte loads of V per lane
+  // V's codes, then {K, V} parameters [NG][64]
+  constexpr int STAGE = kTile * ROW + 2 * NG * kTile * 4;
+  constexpr int OPAD = 36;          // floats of a row of 32 sums in LDS
+  constexpr int SUMS = kWaves * 16 * C * OPAD * 4;
+  constexpr int STATS = kWaves * 16 * C * (2 + NG) * 4;
+  constexpr int LDS = STAGE * kWaves > SUMS ? STAGE * kWaves : SUMS;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[LDS];
+  __shared__ __attribute__((aligned(16))) uint8_t lds_stats[STATS];
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 15, quad = lane >> 4;
+  const int head = blockIdx.x % c.kv_heads;
+  Unit unit;
+  if (!find_unit(b, c.page_shift, u, blockIdx.x / c.kv_heads, -1, &unit)) return;
+  const SeqWork& w = unit.w;
+  const int row0 = unit.block * u.rows;             // of n * group
+  const int rows = min(u.rows, w.n * u.group - row0);
+  // positions of the block's first and last rows
+  const long long pos0 = w.len - w.n + row0 / u.group;
+  const long long pos1 = w.len - w.n + (row0 + rows - 1) / u.group;
+  const long long cap = (long long)b.max_pages << c.page_shift;
+  long long tile0 = w.first + unit.range * unit.per;
+  long long tile1 = min(tile0 + unit.per, (min(pos1 + 1, cap) + kTile - 1) / kTile);
+  if (u.window > 0) tile0 = max(tile0, max(0ll, pos0 - u.window + 1) / kTile);
+
+  // ---- q: operand [step] of each column block, its sums and factor
+  f16x8 q[C][KS];
+  float qsum[C][NG], kappa[C], top[C], weight_sum[C], offset[C][NG];
+  long long pos[C];
+  #pragma unroll
+  for (int cb = 0; cb < C; ++cb) {
+    const int r = 16 * cb + col;
+    const bool live = r < rows;
+    const int i = (row0 + r) / u.group, h = (row0 + r) % u.group;
+    pos[cb] = w.len - w.n + i;
+    const uint16_t* x = a.Q + (long long)(w.start + i) * a.q_stride + (head * u.group + h) * D;
+    u32x4 raw[KS];
+    float big = 0.0f;
+    #pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      // a lane's codes of K: D / 4 channels in a row, or 8 of every 32 where the
+      // steps have to stay within a group
+      const int at = NG == 1 ? D / 4 * quad + 8 * s : 32 * s + 8 * quad;
+      raw[s] = u32x4{0, 0, 0, 0};
+      if (live) raw[s] = *reinterpret_cast<const u32x4*>(x + at);
+      #pragma unroll
+      for (int k = 0; k < 4; ++k)
+        big = fmaxf(big, fmaxf(fabsf(low_half(raw[s][k])), fabsf(low_half(raw[s][k] >> 16))));
+    }
+    big = quad_max(big);
+    int e = 10;
+    if (big > 0.0f && big < INFINITY) e = ilogbf(big);
+    const float f = ldexpf(a.scale < 0.0f ? -1.0f : 1.0f, 10 - e);
+    // above 0, so that an unseen token's -infinity stays one
+    kappa[cb] = fmaxf(ldexpf(fabsf(a.scale) * kLog2e, 24 + e - 10), 0x1p-120f);
+    #pragma unroll
+    for (int g = 0; g < NG; ++g) qsum[cb][g] = 0.0f;
+    #pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      float v[8];
+      float sum = 0.0f;
+      #pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        v[2 * k] = low_half(raw[s][k]) * f;
+        v[2 * k + 1] = low_half(raw[s][k] >> 16) * f;
+        sum += v[2 * k] + v[2 * k + 1];
+      }
+      qsum[cb][32 * s / G % NG] += sum;
+      q[cb][s] = f16x8{(_Float16)v[0],            (_Float16)v[4],
+                       (_Float16)(v[1] * 0.0625f), (_Float16)(v[5] * 0.0625f),
+                       (_Float16)v[2],            (_Float16)v[6],
+                       (_Float16)(v[3] * 0.0625f), (_Float16)(v[7] * 0.0625f)};
+    }
+    #pragma unroll
+    for (int g = 0; g < NG; ++g) qsum[cb][g] = quad_sum(qsum[cb][g]) * 0x1p-24f;
+    top[cb] = kNone;
+    weight_sum[cb] = 0.0f;
+    #pragma unroll
+    for (int g = 0; g < NG; ++g) offset[cb][g] = 0.0f;
+  }
+
+  f32x4 o[C][DB];
+  #pragma unroll
+  for (int cb = 0; cb < C; ++cb)
+    #pragma unroll
+    for (int d = 0; d < DB; ++d) o[cb][d] = f32x4{0, 0, 0, 0};
+  int vexp = -24;  // exponent of the largest scale of V so far
+
+  uint8_t* stage = lds + wave * STAGE;
+  uint32_t* params = reinterpret_cast<uint32_t*>(stage + kTile * ROW);
+
+  // ---- loads of a tile: into registers, a tile ahead
+  uint32_t kreg[4][KS];
+  u32x4 vreg[VL];
+  uint32_t preg[2][NG];
+  bool stored;  // this lane's token (for the parameters) is in the cache
+  const int32_t* table = b.block_table + (long long)unit.seq * b.max_pages;
+
+  auto page_at = [&](long long token) -> int {  // of a 16-token granule
+    const long long i = token >> c.page_shift;
+    if (i >= b.max_pages) return -1;
+    const int page = table[i];
+    return (unsigned)page < (unsigned)c.num_pages ? page : -1;
+  };
+  // first row of the granule's 16 in the cache; a hole reads page 0
+  auto granule_row = [&](int page, long long token) -> long long {
+    return cache_row(c, max(page, 0), head, token);
+  };
+  auto load_k = [&](long long tile) {
+    const long long t = tile * kTile + 16 * (col >> 2);  // the granule of K's row `col`
+    const long long row = granule_row(page_at(t), t) + (col & 3);
+    const uint8_t* at = c.k_codes + row * ROW;
+    #pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint8_t* k = at + 4 * j * ROW;
+      if constexpr (NG == 1) {
+        if constexpr (KS == 4) {
+          const u32x4 v = *reinterpret_cast<const u32x4*>(k + 16 * quad);
+          kreg[j][0] = v[0], kreg[j][1] = v[1], kreg[j][2] = v[2], kreg[j][3] = v[3];
+        } else {
+          const u32x2 v = *reinterpret_cast<const u32x2*>(k + 8 * quad);
+          kreg[j][0] = v[0], kreg[j][1] = v[1];
+        }
+      } else {
+        #pragma unroll
+        for (int s = 0; s < KS; ++s)
+          kreg[j][s] = *reinterpret_cast<const uint32_t*>(k + 16 * s + 4 * quad);
+      }
+    }
+  };
+  auto load_v = [&](long long tile) {
+    const long long t = tile * kTile;
+    #pragma unroll
+    for (int i = 0; i < VL; ++i) {
+      const int token = i * (64 / VL) + lane / VL;
+      const long long tv = t + (token & ~15);
+      const long long row = granule_row(page_at(tv), tv) + (token & 15);
+      vreg[i] = *reinterpret_cast<const u32x4*>(c.v_codes + row * ROW + 16 * (lane % VL));
+    }
+    const long long tp = t + 16 * quad;
+    const int page = page_at(tp);
+    const long long row = granule_row(page, tp) + col;
+    stored = page >= 0 && t + lane < w.len;
+    #pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      preg[0][g] = reinterpret_cast<const uint32_t*>(c.k_params)[row * NG + g];
+      preg[1][g] = reinterpret_cast<const uint32_t*>(c.v_params)[row * NG + g];
+    }
+  };
+
+  // ---- one tile
+  auto work = [&](long long tile, bool whole, unsigned long long held) {
+    f32x4 x[C][4];
+    #pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      f32x4 dot[C];
+      #pragma unroll
+      for (int g = 0; g < NG; ++g) {
+        #pragma unroll
+        for (int cb = 0; cb < C; ++cb) dot[cb] = f32x4{0, 0, 0, 0};
+        #pragma unroll
+        for (int s = g * KS / NG; s < (g + 1) * KS / NG; ++s) {
+          const f16x8 k = codes_f16(kreg[j][s]);
+          #pragma unroll
+          for (int cb = 0; cb < C; ++cb)
+            dot[cb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[cb][s], dot[cb], 0, 0, 0);
+        }
+        if constexpr (NG > 1) __builtin_amdgcn_sched_barrier(0);  // keeps registers few
+        const u32x4 p = *reinterpret_cast<const u32x4*>(params + g * kTile + 16 * quad + 4 * j);
+        #pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float s = low_half(p[r]), mn = low_half(p[r] >> 16);
+          #pragma unroll
+          for (int cb = 0; cb < C; ++cb) {
+            const float more = g ? fmaf(mn, qsum[cb][g], x[cb][j][r]) : mn * qsum[cb][g];
+            x[cb][j][r] = fmaf(s, dot[cb][r], more);
+          }
+        }
+      }
+    }
+    if (tile + kWaves < tile1) load_k(tile + kWaves);
+    if (!whole) {
+      const uint32_t have = (uint32_t)(held >> (16 * quad)) & 0xFFFFu;
+      const long long t = tile * kTile + 16 * quad;
+      #pragma unroll
+      for (int cb = 0; cb < C; ++cb) {
+        // tokens t + k with pos - window < t + k <= pos: bit k
+        const int last = (int)max(-1ll, min(15ll, pos[cb] - t));
+        const int first =
+            u.window > 0 ? (int)max(0ll, min(16ll, pos[cb] - u.window + 1 - t)) : 0;
+        const uint32_t seen = ((1u << (last + 1)) - 1u) & (~0u << first) & have;
+        #pragma unroll
+        for (int k = 0; k < 16; ++k)
+          if (!(seen >> k & 1u)) x[cb][k / 4][k % 4] = -INFINITY;
+      }
+    }
+    // running maximum; what was added up before shrinks with it
+    float next[C];
+    bool grown = false;
+    #pragma unroll
+    for (int cb = 0; cb < C; ++cb) {
+      float m = x[cb][0][0];
+      #pragma unroll
+      for (int k = 1; k < 16; ++k) m = fmaxf(m, x[cb][k / 4][k % 4]);
+      next[cb] = fmaxf(top[cb], quad_max(m) * kappa[cb]);
+      grown |= next[cb] > top[cb];
+    }
+    if (__any(grown)) {
+      #pragma unroll
+      for (int cb = 0; cb < C; ++cb) {
+        const float f = __builtin_amdgcn_exp2f(top[cb] - next[cb]);
+        top[cb] = next[cb];
+        weight_sum[cb] *= f;
+        #pragma unroll
+        for (int g = 0; g < NG; ++g) offset[cb][g] *= f;
+        #pragma unroll
+        for (int d = 0; d < DB; ++d) o[cb][d] *= f;
+      }
+    }
+    #pragma unroll
+    for (int cb = 0; cb < C; ++cb)
+      #pragma unroll
+      for (int j = 0; j < 4; ++j)
+        #pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float p = __builtin_amdgcn_exp2f(fmaf(x[cb][j][r], kappa[cb], -top[cb]));
+          x[cb][j][r] = p;
+          weight_sum[cb] += p;
+        }
+    // the weighted sum, group by group
+    const float unit_even = ldexpf(1.0f, 14 - vexp), unit_odd = unit_even * 0.0625f;
+    #pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      if constexpr (NG > 1) __builtin_amdgcn_sched_barrier(0);
+      f16x8 p[C][2];
+      #pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const u32x4 v0 =
+            *reinterpret_cast<const u32x4*>(params + (NG + g) * kTile + 16 * quad + 8 * h);
+        const u32x4 v1 =
+            *reinterpret_cast<const u32x4*>(params + (NG + g) * kTile + 16 * quad + 8 * h + 4);
+        #pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float unit_r = r & 1 ? unit_odd : unit_even;
+          const float s0 = low_half(v0[r]) * unit_r, s1 = low_half(v1[r]) * unit_r;
+          const float m0 = low_half(v0[r] >> 16), m1 = low_half(v1[r] >> 16);
+          #pragma unroll
+          for (int cb = 0; cb < C; ++cb) {
+            const float w0 = x[cb][2 * h][r], w1 = x[cb][2 * h + 1][r];
+            // the products that are 0 where the weight is, whatever the parameter:
+            // it may be anything for a token that the row does not see
+            offset[cb][g] += mul_zero(w0, m0);
+            offset[cb][g] += mul_zero(w1, m1);
+            p[cb][h][2 * r] = (_Float16)mul_zero(w0, s0);
+            p[cb][h][2 * r + 1] = (_Float16)mul_zero(w1, s1);
+          }
+        }
+      }
+      #pragma unroll
+      for (int d = g * DB / NG; d < (g + 1) * DB / NG; ++d) {
+        // 16-byte chunk d / 2 of token row 16 quad + col, where the store put it
+        const int chunk = VL == 4 ? (d / 2) ^ (col >> 2) : (d / 2) ^ (col >> 3);
+        const uint8_t* at = stage + (16 * quad + col) * ROW + 16 * chunk + 8 * (d & 1);
+        const i32x2 v = __builtin_amdgcn_ds_read_tr4_b64_v2i32(
+            (__attribute__((address_space(3))) i32x2*)at);
+        #pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const f16x8 vc = codes_f16((uint32_t)v[h]);
+          #pragma unroll
+          for (int cb = 0; cb < C; ++cb)
+            o[cb][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vc, p[cb][h], o[cb][d], 0, 0, 0);
+        }
+      }
+    }
+  };
+
+  const long long first = tile0 + wave;
+  if (first < tile1) {
+    load_k(first);
+    load_v(first);
+  }
+  for (long long tile = first; tile < tile1; tile += kWaves) {
+    // ---- V and the parameters into LDS; tokens that are not there have none
+    uint32_t big = 0;
+    #pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      const uint32_t kp = stored ? preg[0][g] : 0u, vp = stored ? preg[1][g] : 0u;
+      params[g * kTile + lane] = kp;
+      params[(NG + g) * kTile + lane] = vp;
+      const uint32_t s = vp & 0xFFFFu;
+      big = max(big, s < 0x7C00u ? s : 0u);  // finite scales, as bits
+    }
+    #pragma unroll
+    for (int i = 0; i < VL; ++i) {
+      const int token = i * (64 / VL) + lane / VL;
+      // chunks in turned order, so that the 16 rows of a transposing read lie in
+      // different banks
+      const int chunk = lane % VL ^ (VL == 4 ? (token >> 2) & 3 : (token >> 3) & 1);
+      *reinterpret_cast<u32x4*>(stage + token * ROW + 16 * chunk) = vreg[i];
+    }
+    const unsigned long long held = __ballot(stored);
+    // the largest scale sets the unit of the weights
+    const float vbig = low_half(big);
+    if (__any(vbig >= ldexpf(1.0f, vexp + 1))) {
+      float m = vbig;
+      #pragma unroll
+      for (int s = 1; s < 64; s <<= 1) m = fmaxf(m, __shfl_xor(m, s));
+      const int e = ilogbf(m);
+      const float f = ldexpf(1.0f, vexp - e);
+      vexp = e;
+      #pragma unroll
+      for (int cb = 0; cb < C; ++cb)
+        #pragma unroll
+        for (int d = 0; d < DB; ++d) o[cb][d] *= f;
+    }
+    if (tile + kWaves < tile1) load_v(tile + kWaves);
+    // LDS is this wave's own: its accesses stay in order
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    const long long t = tile * kTile;
+    const bool whole = held == ~0ull && t + kTile - 1 <= pos0 &&
+                       (u.window == 0 || t > pos1 - u.window);
+    work(tile, whole, held);
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  }
+
+  // ---- the four waves' results together
+  float* stats = reinterpret_cast<float*>(lds_stats);  // [wave][16 C][2 + NG]
+  #pragma unroll
+  for (int cb = 0; cb < C; ++cb) {
+    float* at = stats + (wave * 16 * C + 16 * cb + col) * (2 + NG);
+    const float sum = quad_sum(weight_sum[cb]);
+    if (quad == 0) {
+      at[0] = top[cb];
+      at[1] = sum;
+    }
+    #pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      const float v = quad_sum(offset[cb][g]);
+      if (quad == 0) at[2 + g] = v;
+    }
+  }
+  __syncthreads();
+  // factor of this wave's sums; then everything relative to the common maximum
+  float factor[C];
+  #pragma unroll
+  for (int cb = 0; cb < C; ++cb) {
+    float m = kNone;
+    #pragma unroll
+    for (int k = 0; k < kWaves; ++k)
+      m = fmaxf(m, stats[(k * 16 * C + 16 * cb + col) * (2 + NG)]);
+    factor[cb] = ldexpf(__builtin_amdgcn_exp2f(top[cb] - m), 24 - 14 + vexp);
+  }
+  // a thread adds up two channels of C rows, 32 channels of all rows at a time
+  const int my_row = threadIdx.x >> 4, my_channel = 2 * (threadIdx.x & 15);
+  float my_top[C], my_sum[C], my_offset[C][NG];
+  #pragma unroll
+  for (int cb = 0; cb < C; ++cb) {
+    float m = kNone;
+    #pragma unroll
+    for (int k = 0; k < kWaves; ++k)
+      m = fmaxf(m, stats[(k * 16 * C + 16 * cb + my_row) * (2 + NG)]);
+    my_top[cb] = m;
+    my_sum[cb] = 0.0f;
+    #pragma unroll
+    for (int g = 0; g < NG; ++g) my_offset[cb][g] = 0.0f;
+    #pragma unroll
+    for (int k = 0; k < kWaves; ++k) {
+      const float* at = stats + (k * 16 * C + 16 * cb + my_row) * (2 + NG);
+      const float f = __builtin_amdgcn_exp2f(at[0] - m);
+      my_sum[cb] += f * at[1];
+      #pragma unroll
+      for (int g = 0; g < NG; ++g) my_offset[cb][g] += f * at[2 + g];
+    }
+  }
+  float* sums = reinterpret_cast<float*>(lds);  // [wave][16 C][OPAD]
+  #pragma unroll
+  for (int d = 0; d < D / 32; ++d) {
+    __syncthreads();
+    #pragma unroll
+    for (int cb = 0; cb < C; ++cb)
+      #pragma unroll
+      for (int k = 0; k < 2; ++k)
+        *reinterpret_cast<f32x4*>(sums + (wave * 16 * C + 16 * cb + col) * OPAD + 16 * k +
+                                  4 * quad) = o[cb][2 * d + k] * factor[cb];
+    __syncthreads();
+    #pragma unroll
+    for (int cb = 0; cb < C; ++cb) {
+      const int r = 16 * cb + my_row;
+      const float off = my_offset[cb][32 * d / G];
+      f32x2 v = {off, off};
+      #pragma unroll
+      for (int k = 0; k < kWaves; ++k)
+        v += *reinterpret_cast<const f32x2*>(sums + (k * 16 * C + r) * OPAD + my_channel);
+      if (r >= rows) continue;
+      if (unit.ranges > 1) {
+        if (unit.slot >= part.slots) continue;  // no batch that comet.h allows
+        const long long at = ((long long)unit.slot * c.kv_heads + head) * u.rows + r;
+        *reinterpret_cast<f32x2*>(part.sums + at * D + 32 * d + my_channel) = v;
+        if (d == 0 && my_channel == 0)
+          *reinterpret_cast<f32x2*>(part.stats + at * 2) = f32x2{my_top[cb], my_sum[cb]};
+      } else {
+        const float f = my_sum[cb] != 0.0f ? 1.0f / my_sum[cb] : 0.0f;
+        const int i = (row0 + r) / u.group, h = (row0 + r) % u.group;
+        const f16x2 y = {(_Float16)(v[0] * f), (_Float16)(v[1] * f)};
+        *reinterpret_cast<f16x2*>(a.out + (long long)(w.start + i) * a.out_stride +
+                                  (head * u.group + h) * D + 32 * d + my_channel) = y;
+      }
+    }
+  }
+}
+
+// Adds up the ranges of rows that have several: a block takes one row of q and a
+// few of its heads, a thread four channels of one head.
+__global__ __launch_bounds__(256) void kv4_attention_combine_kernel(PagedCache c, PagedBatch b,
+                                                                    AttentionArgs a, UnitShape u,
+                                                                    Partials part) {
   const int m = blockIdx.x;
   int seq;
   long long p;
   if (!find_row(b, m, &seq, &p)) return;
-  const int D = c.head_dim, G = c.G, head = h / (a.heads / c.kv_heads);
-  const uint16_t* x = a.Q + (long long)m * a.q_stride + h * D;
-  for (int i = lane; i < D; i += 64) q[i] = low_half(x[i]);
-  __syncthreads();
-  const long long end = min(p + 1, (long long)b.max_pages << c.page_shift);
-  const long long begin = a.window > 0 ? max(0ll, p - a.window + 1) : 0;
-  float top = -INFINITY, sum = 0.0f, o0 = 0.0f, o1 = 0.0f;
-  for (long long j0 = begin; j0 < end; j0 += 64) {
-    const long long j = j0 + lane;
-    const int page = j < end ? token_page(b, seq, j, c.page_shift, c.num_pages) : -1;
-    float score = -INFINITY;
-    if (page >= 0) {
-      const long long row = cache_row(c, page, head, j);
-      const uint32_t* codes = reinterpret_cast<const uint32_t*>(c.k_codes) + row * (D / 8);
-      const uint32_t* params = reinterpret_cast<const uint32_t*>(c.k_params) + row * (D / G);
-      score = 0.0f;
-      for (int g = 0; g < D / G; ++g) {
-        float dot = 0.0f, qs = 0.0f;
-        for (int w = 0; w < G / 8; ++w) {
-          const uint32_t v = codes[g * (G / 8) + w];
-          #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float e = q[g * G + 8 * w + i];
-            dot = fmaf((float)((v >> (4 * i)) & 15u), e, dot);
-            qs += e;
-          }
-        }
-        score += low_half(params[g]) * dot + low_half(params[g] >> 16) * qs;
-      }
-      score *= a.scale * kLog2e;
-    }
-    const float next = fmaxf(top, wave_max(score));
-    const float shrink = next == top ? 1.0f : exp2f(top - next);
-    const float w = page >= 0 ? exp2f(score - next) : 0.0f;
-    __syncthreads();
-    weight[lane] = w;
-    pages[lane] = page;
-    __syncthreads();
-    sum = sum * shrink + wave_sum(w);
-    top = next;
-    o0 *= shrink;
-    o1 *= shrink;
-    const int n = (int)min(64ll, end - j0);
-    if (lane < D / 2) {
-      for (int t = 0; t < n; ++t) {
-        if (pages[t] < 0) continue;
-        const long long row = cache_row(c, pages[t], head, j0 + t);
-        const uint32_t v = c.v_codes[row * (D / 2) + lane];
-        const uint32_t param =
-            reinterpret_cast<const uint32_t*>(c.v_params)[row * (D / G) + 2 * lane / G];
-        const float s = low_half(param), mn = low_half(param >> 16);
-        o0 = fmaf(weight[t], fmaf((float)(v & 15u), s, mn), o0);
-        o1 = fmaf(weight[t], fmaf((float)(v >> 4), s, mn), o1);
-      }
-    }
+  Unit unit;
+  if (!find_unit(b, c.page_shift, u, 0, seq, &unit) || unit.ranges < 2) return;
+  const int D = c.head_dim, lanes = D / 4;
+  const int head = blockIdx.y * (256 / lanes) + threadIdx.x / lanes;
+  if (head >= a.heads) return;
+  const int channel = 4 * (threadIdx.x % lanes);
+  const long long r = (long long)(m - unit.w.start) * u.group + head % u.group;
+  const long long block = unit.w.blocks - 1 - r / u.rows;
+  const long long slot = unit.slot + block * unit.ranges;
+  if (slot + unit.ranges > part.slots) return;  // no batch that comet.h allows
+  // row of the first range's result; the next ranges' lie `step` apart
+  const long long first = (slot * c.kv_heads + head / u.group) * u.rows + r % u.rows;
+  const long long step = (long long)c.kv_heads * u.rows;
+  float top = kNone;
+  for (int k = 0; k < unit.ranges; ++k) top = fmaxf(top, part.stats[(first + k * step) * 2]);
+  float sum = 0.0f;
+  f32x4 v = {0, 0, 0, 0};
+  for (int k = 0; k < unit.ranges; ++k) {
+    const long long at = first + k * step;
+    const float f = __builtin_amdgcn_exp2f(part.stats[at * 2] - top);
+    sum += f * part.stats[at * 2 + 1];
+    v += f * *reinterpret_cast<const f32x4*>(part.sums + at * D + channel);
   }
-  if (lane < D / 2) {
-    const float r = sum != 0.0f ? 1.0f / sum : 0.0f;
-    const uint32_t lo = __half_as_ushort(__float2half_rn(o0 * r));
-    const uint32_t hi = __half_as_ushort(__float2half_rn(o1 * r));
-    reinterpret_cast<uint32_t*>(a.out + (long long)m * a.out_stride + h * D)[lane] = lo | hi << 16;
-  }
+  const float f = sum != 0.0f ? 1.0f / sum : 0.0f;
+  const f16x2 y[2] = {{(_Float16)(v[0] * f), (_Float16)(v[1] * f)},
+                      {(_Float16)(v[2] * f), (_Float16)(v[3] * f)}};
+  *reinterpret_cast<u32x2*>(a.out + (long long)m * a.out_stride + head * D + channel) =
+      __builtin_bit_cast(u32x2, *reinterpret_cast<const u32x2*>(y));
+}
+
+// ---- host ------------------------------------------------------------------------
+
+struct Shape {
+  UnitShape u;
+  int columns;       // C
+  long long blocks;  // of the grid: units that a batch of these sizes may have, times kv heads
+  long long slots;   // partial results
+};
+
+Shape shape_of(const PagedCache& c, const PagedBatch& b, int heads, int window, int cus) {
+  Shape s;
+  s.u.group = heads / c.kv_heads;
+  s.columns = (long long)b.max_rows * s.u.group > 16 ? 2 : 1;
+  s.u.rows = 16 * s.columns;
+  s.u.window = window;
+  // blocks that a compute unit holds at a time
+  const int resident = s.columns == 1 ? 3 : 2;
+  s.u.target = std::max(1, cus * resident / c.kv_heads);
+  // every sequence's last row block may be ragged
+  const long long row_blocks =
+      (long long)b.M * s.u.group / s.u.rows + std::min(b.B, b.M);
+  const long long tiles = (((long long)b.max_pages << c.page_shift) + kTile - 1) / kTile;
+  const long long ranges = (tiles + kMinTiles - 1) / kMinTiles;
+  s.slots = ranges > 1 ? std::min<long long>(2 * s.u.target, row_blocks * ranges) : 0;
+  s.blocks = std::min(row_blocks + s.u.target, row_blocks * ranges) * c.kv_heads;
+  return s;
+}
+
+template <int D, int G>
+void launch_columns(const PagedCache& c, const PagedBatch& b, const AttentionArgs& a,
+                    const Shape& s, const Partials& part, hipStream_t stream) {
+  const dim3 grid((unsigned)s.blocks), block(64 * kWaves);
+  if (s.columns == 1)
+    hipLaunchKernelGGL((kv4_attention_kernel<D, G, 1>), grid, block, 0, stream, c, b, a, s.u, part);
+  else
+    hipLaunchKernelGGL((kv4_attention_kernel<D, G, 2>), grid, block, 0, stream, c, b, a, s.u, part);
 }
 
 }  // namespace
 
-size_t attention_workspace(const PagedCache&, const PagedBatch&, int, int) { return 0; }
+const char* attention_refusal(const PagedCache& c, const PagedBatch& b, int heads, int cus) {
+  // a launch's threads are counted in 32 bits
+  const Shape s = shape_of(c, b, heads, 0, cus);
+  return s.blocks >= (1ll << 32) / (64 * kWaves) ? "too many rows, heads and sequences for a launch"
+                                                 : nullptr;
+}
+
+size_t attention_workspace(const PagedCache& c, const PagedBatch& b, int heads, int cus) {
+  const Shape s = shape_of(c, b, heads, 0, cus);
+  return (size_t)s.slots * c.kv_heads * s.u.rows * (c.head_dim + 2) * sizeof(float);
+}
 
 hipError_t launch_kv4_attention(const PagedCache& c, const PagedBatch& b, const AttentionArgs& a,
                                 hipStream_t stream) {
-  hipLaunchKernelGGL(kv4_attention_row_kernel, dim3(b.M, a.heads), dim3(64), 0, stream, c, b, a);
+  const Shape s = shape_of(c, b, a.heads, a.window, a.cus);
+  float* ws = static_cast<float*>(a.workspace);
+  const Partials part{ws, ws + s.slots * c.kv_heads * s.u.rows * c.head_dim, (uint32_t)s.slots};
+  if (c.head_dim == 128 && c.G == 128)
+    launch_columns<128, 128>(c, b, a, s, part, stream);
+  else if (c.head_dim == 128 && c.G == 64)
+    launch_columns<128, 64>(c, b, a, s, part, stream);
+  else if (c.head_dim == 128)
+    launch_columns<128, 32>(c, b, a, s, part, stream);
+  else if (c.G == 64)
+    launch_columns<64, 64>(c, b, a, s, part, stream);
+  else
+    launch_columns<64, 32>(c, b, a, s, part, stream);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !s.slots) return e;
+  const int heads = 256 / (c.head_dim / 4);
+  hipLaunchKernelGGL(kv4_attention_combine_kernel, dim3(b.M, (a.heads + heads - 1) / heads),
+                     dim3(256), 0, stream, c, b, a, s.u, part);
   return hipGetLastError();
 }
 

@@ -67,6 +67,8 @@ struct AttentionArgs {
   void* workspace;
   int cus;
 };
+// nullptr, or why these sizes cannot run.
+const char* attention_refusal(const PagedCache& c, const PagedBatch& b, int heads, int cus);
 size_t attention_workspace(const PagedCache& c, const PagedBatch& b, int heads, int cus);
 hipError_t launch_kv4_attention(const PagedCache& c, const PagedBatch& b, const AttentionArgs& a,
                                 hipStream_t stream);
