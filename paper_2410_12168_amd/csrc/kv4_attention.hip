@@ -65,14 +65,52 @@ __device__ inline float low_half(uint32_t w) {
   return __half2float(__ushort_as_half((unsigned short)w));
 }
 
-// Sum and maximum over the four lanes of a column (l, l ^ 16, l ^ 32, l ^ 48).
+// Rows of 16 lanes: the odd rows of a change places with the even rows of b
+// (swap16), or a's upper half with b's lower (swap32).
+__device__ inline void swap16(uint32_t& a, uint32_t& b) {
+  const auto r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+  a = r[0];
+  b = r[1];
+}
+__device__ inline void swap32(uint32_t& a, uint32_t& b) {
+  const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+  a = r[0];
+  b = r[1];
+}
+
+// Maximum and sum over the four lanes of a column (l, l ^ 16, l ^ 32, l ^ 48).
+template <typename F>
+__device__ inline float over_quads(float v, F f) {
+  uint32_t a = __float_as_uint(v), b = a;
+  swap16(a, b);
+  v = f(__uint_as_float(a), __uint_as_float(b));
+  a = b = __float_as_uint(v);
+  swap32(a, b);
+  return f(__uint_as_float(a), __uint_as_float(b));
+}
 __device__ inline float quad_max(float v) {
-  v = fmaxf(v, __shfl_xor(v, 16));
-  return fmaxf(v, __shfl_xor(v, 32));
+  return over_quads(v, [](float a, float b) { return fmaxf(a, b); });
 }
 __device__ inline float quad_sum(float v) {
-  v += __shfl_xor(v, 16);
-  return v + __shfl_xor(v, 32);
+  return over_quads(v, [](float a, float b) { return a + b; });
+}
+
+// Sums over the lanes up to each (the last lane has all 64), without LDS: shifts
+// within rows of 16, then the last lanes of rows 0 and 2, then of row 1.
+template <int CTRL, int ROWS, typename T>
+__device__ inline T shifted(T v) {
+  return __builtin_bit_cast(
+      T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, ROWS, 0xF, ROWS == 0xF));
+}
+template <typename T>
+__device__ inline T sum_upto(T v) {
+  v += shifted<0x111, 0xF>(v);
+  v += shifted<0x112, 0xF>(v);
+  v += shifted<0x114, 0xF>(v);
+  v += shifted<0x118, 0xF>(v);
+  v += shifted<0x142, 0xA>(v);
+  v += shifted<0x143, 0xC>(v);
+  return v;
 }
 
 // a * b, and 0 where either is 0 whatever the other is (v_mul_legacy_f32).
@@ -96,11 +134,11 @@ struct UnitShape {
 };
 
 struct SeqWork {
-  int start, n;        // first row, rows
-  long long len;       // tokens
-  long long blocks;    // row blocks
-  long long first;     // first tile that any row sees
-  long long tiles;     // tiles from there on (1 at least)
+  int start, n;    // first row, rows
+  int len;         // tokens
+  uint32_t blocks; // row blocks
+  uint32_t first;  // first tile that any row sees
+  uint32_t tiles;  // tiles from there on (1 at least)
 };
 
 __device__ inline SeqWork seq_work(const PagedBatch& b, int page_shift, const UnitShape& u,
@@ -109,109 +147,94 @@ __device__ inline SeqWork seq_work(const PagedBatch& b, int page_shift, const Un
   if (seq >= b.B) return w;
   w.start = max(0, min(b.M, b.row_start[seq]));
   w.n = max(0, max(0, min(b.M, b.row_start[seq + 1])) - w.start);
-  w.len = b.seq_lens[seq];
-  const long long cap = (long long)b.max_pages << page_shift;
-  const long long seen = max(0ll, min(w.len, cap));
-  const long long low = u.window > 0 ? max(0ll, w.len - w.n - u.window + 1) : 0ll;
-  w.blocks = ((long long)w.n * u.group + u.rows - 1) / u.rows;
-  w.first = low / kTile;
-  w.tiles = max(1ll, (seen + kTile - 1) / kTile - w.first);
+  w.len = max(-b.M, min(1 << 30, b.seq_lens[seq]));
+  const int seen = max(0, min(w.len, b.max_pages << page_shift));  // 2^30 at most
+  const int low = w.len - w.n - u.window + 1;                       // of the first row's window
+  w.blocks = ((uint32_t)w.n * u.group + u.rows - 1) / u.rows;
+  w.first = u.window > 0 ? max(0, low) / kTile : 0;
+  w.tiles = max(1, (seen + kTile - 1) / kTile - (int)w.first);
   return w;
 }
 
-// One block's work: row block `block` of sequence `seq`, range `range` of `ranges`
-// with `per` tiles each.
+// One block's work: row block `block` of sequence `seq`, range `range` of
+// `ranges`, in which the sequence's tiles are shared out evenly.
 struct Unit {
-  int seq, block, range, ranges;
-  long long per;
-  uint32_t before;   // units of earlier sequences
-  uint32_t slot;     // partial results of earlier sequences
+  int seq;
+  uint32_t block, range, ranges;
+  uint32_t slot;  // of the partial result
   SeqWork w;
 };
 
 // Lane `at`'s value (`at` the same in all lanes) where the compiler knows that all
 // lanes have it.
-__device__ inline int from_lane(int v, int at) { return __builtin_amdgcn_readlane(v, at); }
-__device__ inline long long from_lane(long long v, int at) {
-  const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, at);
-  const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), at);
-  return (long long)((unsigned long long)hi << 32 | lo);
-}
-
 template <typename T>
-__device__ inline T wave_sum(T v) {
-  #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
-  return v;
+__device__ inline T from_lane(T v, int at) {
+  return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), at));
 }
 
-// Tiles of a range, from the work of all sequences: the same in every wave of a
-// launch.
-__device__ inline long long tiles_per_range(const PagedBatch& b, int page_shift,
-                                            const UnitShape& u) {
+// Tiles of a range at most, from the work of all sequences: the same in every wave
+// of a launch.  Rounded up by more than the 32-bit sum can be off, so that the
+// ranges of full length are `target` at most.
+__device__ inline float tiles_per_range(const PagedBatch& b, int page_shift, const UnitShape& u) {
   const int lane = threadIdx.x & 63;
-  double total = 0.0;  // whole numbers, exact
+  float total = 0.0f;
   for (int s = 0; s < b.B; s += 64) {
     const SeqWork w = seq_work(b, page_shift, u, s + lane);
-    total += (double)w.blocks * (double)w.tiles;
+    total += (float)w.blocks * (float)w.tiles;
   }
-  return from_lane(max((long long)kMinTiles, (long long)ceil(wave_sum(total) / u.target)), 0);
+  total = from_lane(sum_upto(total), 63) * 1.001f;
+  return fmaxf((float)kMinTiles, ceilf(total / (float)u.target));
 }
 
-// Unit `index` (counted over sequences, row blocks and ranges), or the units
-// before sequence `want` (want >= 0).  False if there is none.  Both counts, of
-// all units and of those that leave partial results, run in one sum of 32 + 32
-// bits.
+__device__ inline uint32_t ranges_of(const SeqWork& w, float per) {
+  return (uint32_t)ceilf((float)w.tiles / per);
+}
+
+// Unit `index`, counted over sequences, row blocks and ranges (SPLIT: row block
+// `index` of those whose sequence has more than one range).  False if there is
+// none.  Sums of 32 bits: more than a launch can have only in batches that the
+// interface does not allow, whose units are then any or none of the batch's.
+template <bool SPLIT>
 __device__ inline bool find_unit(const PagedBatch& b, int page_shift, const UnitShape& u,
-                                 uint32_t index, int want, Unit* out) {
+                                 uint32_t index, Unit* out) {
   const int lane = threadIdx.x & 63;
-  const long long per = tiles_per_range(b, page_shift, u);
-  long long before = 0;
+  const float per = tiles_per_range(b, page_shift, u);
+  uint32_t before = 0, slots_before = 0;
   for (int s = 0; s < b.B; s += 64) {
     const SeqWork w = seq_work(b, page_shift, u, s + lane);
-    const long long ranges = (w.tiles + per - 1) / per;
-    long long mine = w.blocks * ranges;
-    if (ranges > 1) mine |= mine << 32;
-    long long upto = mine;
-    #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const long long v = __shfl_up(upto, o);
-      if (lane >= o) upto += v;
-    }
-    const bool here = want >= 0 ? s + lane == want : (uint32_t)(before + upto) > index;
-    const unsigned long long hit = __ballot(here);
+    const uint32_t ranges = ranges_of(w, per);
+    const uint32_t slots = ranges > 1 ? w.blocks * ranges : 0;
+    const uint32_t mine = SPLIT ? (ranges > 1 ? w.blocks : 0) : w.blocks * ranges;
+    const uint32_t upto = before + sum_upto(mine), slots_upto = slots_before + sum_upto(slots);
+    const unsigned long long hit = __ballot(mine > 0 && upto > index);
     if (hit) {
       const int at = __builtin_amdgcn_readfirstlane(__ffsll((long long)hit) - 1);
-      const long long sum = before + from_lane(upto - mine, at);
+      const uint32_t k = index - from_lane(upto - mine, at);
       out->seq = s + at;
-      out->per = per;
-      out->before = (uint32_t)sum;
-      out->slot = (uint32_t)(sum >> 32);
-      out->ranges = (int)from_lane(ranges, at);
+      out->ranges = from_lane(ranges, at);
       out->w.start = from_lane(w.start, at);
       out->w.n = from_lane(w.n, at);
       out->w.len = from_lane(w.len, at);
       out->w.blocks = from_lane(w.blocks, at);
       out->w.first = from_lane(w.first, at);
       out->w.tiles = from_lane(w.tiles, at);
-      if (want < 0) {
-        const uint32_t k = index - out->before;
-        // the last row blocks see the most tokens: they come first
-        out->block = (int)(out->w.blocks - 1 - k / (uint32_t)out->ranges);
-        out->range = (int)(k % (uint32_t)out->ranges);
-        out->slot += k;
-      }
+      const uint32_t block = SPLIT ? k : k / out->ranges;
+      out->range = SPLIT ? 0 : k % out->ranges;
+      out->slot = from_lane(slots_upto - slots, at) + block * out->ranges + out->range;
+      // the last row blocks see the most tokens: they come first
+      out->block = out->w.blocks - 1 - block;
       return true;
     }
-    before += from_lane(upto, 63);
+    before = from_lane(upto, 63);
+    slots_before = from_lane(slots_upto, 63);
   }
   return false;
 }
 
 // Partial results in the workspace: [slot][kv head][rows][D] sums and
 // [slot][kv head][rows][2] {maximum (log2), sum of weights}.  A sequence with more
-// than one range has more than `per` tiles, and `per` is at least all tiles over
-// `target`: there are fewer than 2 * target slots.
+// than one range has more tiles than the longest range may have, which is at
+// least all tiles over `target`: there are fewer than 2 * target slots.
 struct Partials {
   float* sums;
   float* stats;
@@ -228,8 +251,8 @@ __global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_ker
   constexpr int DB = D / 16;        // 16-channel blocks of the output
   constexpr int ROW = D / 2;        // bytes of a row of codes
   constexpr int VL = ROW / 16;      // 16-byte loads of V per lane
-  // V's codes, then {K, V} parameters [NG][64]
-  constexpr int STAGE = kTile * ROW + 2 * NG * kTile * 4;
+  // V's codes, then the parameters in 32 bits: [NG][K's s, mn, V's s, mn][64]
+  constexpr int STAGE = kTile * ROW + 4 * NG * kTile * 4;
   constexpr int OPAD = 36;          // floats of a row of 32 sums in LDS
   constexpr int SUMS = kWaves * 16 * C * OPAD * 4;
   constexpr int STATS = kWaves * 16 * C * (2 + NG) * 4;
@@ -241,22 +264,28 @@ __global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_ker
   const int col = lane & 15, quad = lane >> 4;
   const int head = blockIdx.x % c.kv_heads;
   Unit unit;
-  if (!find_unit(b, c.page_shift, u, blockIdx.x / c.kv_heads, -1, &unit)) return;
+  if (!find_unit<false>(b, c.page_shift, u, blockIdx.x / c.kv_heads, &unit)) return;
   const SeqWork& w = unit.w;
   const int row0 = unit.block * u.rows;             // of n * group
   const int rows = min(u.rows, w.n * u.group - row0);
   // positions of the block's first and last rows
-  const long long pos0 = w.len - w.n + row0 / u.group;
-  const long long pos1 = w.len - w.n + (row0 + rows - 1) / u.group;
-  const long long cap = (long long)b.max_pages << c.page_shift;
-  long long tile0 = w.first + unit.range * unit.per;
-  long long tile1 = min(tile0 + unit.per, (min(pos1 + 1, cap) + kTile - 1) / kTile);
-  if (u.window > 0) tile0 = max(tile0, max(0ll, pos0 - u.window + 1) / kTile);
+  const int pos0 = w.len - w.n + row0 / u.group;
+  const int pos1 = w.len - w.n + (row0 + rows - 1) / u.group;
+  const int cap = b.max_pages << c.page_shift;
+  // the unit's share of the sequence's tiles, without those its rows do not see
+  const uint32_t each = w.tiles / unit.ranges, more = w.tiles % unit.ranges;
+  int tile0 = w.first + unit.range * each + min(unit.range, more);
+  int tile1 = tile0 + each + (unit.range < more);
+  if (pos1 < 0)
+    tile1 = 0;
+  else
+    tile1 = min(tile1, min(pos1, cap - 1) / kTile + 1);
+  if (u.window > 0) tile0 = max(tile0, max(0, pos0 - u.window + 1) / kTile);
 
   // ---- q: operand [step] of each column block, its sums and factor
   f16x8 q[C][KS];
   float qsum[C][NG], kappa[C], top[C], weight_sum[C], offset[C][NG];
-  long long pos[C];
+  int pos[C];
   #pragma unroll
   for (int cb = 0; cb < C; ++cb) {
     const int r = 16 * cb + col;
@@ -269,8 +298,10 @@ __global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_ker
     #pragma unroll
     for (int s = 0; s < KS; ++s) {
       // a lane's codes of K: D / 4 channels in a row, or 8 of every 32 where the
-      // steps have to stay within a group
-      const int at = NG == 1 ? D / 4 * quad + 8 * s : 32 * s + 8 * quad;
+      // steps have to stay within a group (as load_k's rows are turned)
+      const int at = NG == 1 ? D / 4 * quad + 8 * s
+                     : KS == 4 ? 32 * s + 8 * quad
+                               : 32 * s + 16 * (quad & 1) + 8 * (quad >> 1);
       raw[s] = u32x4{0, 0, 0, 0};
       if (live) raw[s] = *reinterpret_cast<const u32x4*>(x + at);
       #pragma unroll
@@ -315,9 +346,10 @@ __global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_ker
     #pragma unroll
     for (int d = 0; d < DB; ++d) o[cb][d] = f32x4{0, 0, 0, 0};
   int vexp = -24;  // exponent of the largest scale of V so far
+  float weight_unit = ldexpf(1.0f, (lane & 1 ? 10 : 14) - vexp);
 
   uint8_t* stage = lds + wave * STAGE;
-  uint32_t* params = reinterpret_cast<uint32_t*>(stage + kTile * ROW);
+  float* params = reinterpret_cast<float*>(stage + kTile * ROW);
 
   // ---- loads of a tile: into registers, a tile ahead
   uint32_t kreg[4][KS];
@@ -326,49 +358,39 @@ __global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_ker
   bool stored;  // this lane's token (for the parameters) is in the cache
   const int32_t* table = b.block_table + (long long)unit.seq * b.max_pages;
 
-  auto page_at = [&](long long token) -> int {  // of a 16-token granule
-    const long long i = token >> c.page_shift;
+  auto page_at = [&](int token) -> int {  // of a 16-token granule
+    const int i = token >> c.page_shift;
     if (i >= b.max_pages) return -1;
     const int page = table[i];
     return (unsigned)page < (unsigned)c.num_pages ? page : -1;
   };
   // first row of the granule's 16 in the cache; a hole reads page 0
-  auto granule_row = [&](int page, long long token) -> long long {
+  auto granule_row = [&](int page, int token) -> long long {
     return cache_row(c, max(page, 0), head, token);
   };
-  auto load_k = [&](long long tile) {
-    const long long t = tile * kTile + 16 * (col >> 2);  // the granule of K's row `col`
-    const long long row = granule_row(page_at(t), t) + (col & 3);
-    const uint8_t* at = c.k_codes + row * ROW;
+  auto load_k = [&](int tile) {
+    const int t = tile * kTile + 16 * (col >> 2);  // the granule of K's row `col`
+    const uint8_t* at = c.k_codes + (granule_row(page_at(t), t) + (col & 3)) * ROW + ROW / 4 * quad;
     #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const uint8_t* k = at + 4 * j * ROW;
-      if constexpr (NG == 1) {
-        if constexpr (KS == 4) {
-          const u32x4 v = *reinterpret_cast<const u32x4*>(k + 16 * quad);
-          kreg[j][0] = v[0], kreg[j][1] = v[1], kreg[j][2] = v[2], kreg[j][3] = v[3];
-        } else {
-          const u32x2 v = *reinterpret_cast<const u32x2*>(k + 8 * quad);
-          kreg[j][0] = v[0], kreg[j][1] = v[1];
-        }
+      if constexpr (KS == 4) {
+        const u32x4 v = *reinterpret_cast<const u32x4*>(at + 4 * j * ROW);
+        kreg[j][0] = v[0], kreg[j][1] = v[1], kreg[j][2] = v[2], kreg[j][3] = v[3];
       } else {
-        #pragma unroll
-        for (int s = 0; s < KS; ++s)
-          kreg[j][s] = *reinterpret_cast<const uint32_t*>(k + 16 * s + 4 * quad);
+        const u32x2 v = *reinterpret_cast<const u32x2*>(at + 4 * j * ROW);
+        kreg[j][0] = v[0], kreg[j][1] = v[1];
       }
     }
   };
-  auto load_v = [&](long long tile) {
-    const long long t = tile * kTile;
+  auto load_v = [&](int tile) {
+    const int t = tile * kTile;
     #pragma unroll
     for (int i = 0; i < VL; ++i) {
-      const int token = i * (64 / VL) + lane / VL;
-      const long long tv = t + (token & ~15);
+      const int token = i * (64 / VL) + lane / VL, tv = t + (token & ~15);
       const long long row = granule_row(page_at(tv), tv) + (token & 15);
       vreg[i] = *reinterpret_cast<const u32x4*>(c.v_codes + row * ROW + 16 * (lane % VL));
     }
-    const long long tp = t + 16 * quad;
-    const int page = page_at(tp);
+    const int tp = t + 16 * quad, page = page_at(tp);
     const long long row = granule_row(page, tp) + col;
     stored = page >= 0 && t + lane < w.len;
     #pragma unroll
@@ -379,11 +401,19 @@ __global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_ker
   };
 
   // ---- one tile
-  auto work = [&](long long tile, bool whole, unsigned long long held) {
+  auto work = [&](int tile, bool whole, unsigned long long held) {
     f32x4 x[C][4];
     #pragma unroll
     for (int j = 0; j < 4; ++j) {
       f32x4 dot[C];
+      if constexpr (NG > 1 && KS == 4) {  // 16 channels of a quad's 4 loads -> of 4 quads
+        swap32(kreg[j][0], kreg[j][2]);
+        swap32(kreg[j][1], kreg[j][3]);
+        swap16(kreg[j][0], kreg[j][1]);
+        swap16(kreg[j][2], kreg[j][3]);
+      } else if constexpr (NG > 1) {
+        swap32(kreg[j][0], kreg[j][1]);
+      }
       #pragma unroll
       for (int g = 0; g < NG; ++g) {
         #pragma unroll
@@ -396,28 +426,32 @@ __global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_ker
             dot[cb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[cb][s], dot[cb], 0, 0, 0);
         }
         if constexpr (NG > 1) __builtin_amdgcn_sched_barrier(0);  // keeps registers few
-        const u32x4 p = *reinterpret_cast<const u32x4*>(params + g * kTile + 16 * quad + 4 * j);
+        const float* at = params + 4 * g * kTile + 16 * quad + 4 * j;
+        const f32x4 s = *reinterpret_cast<const f32x4*>(at);
+        const f32x4 mn = *reinterpret_cast<const f32x4*>(at + kTile);
         #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const float s = low_half(p[r]), mn = low_half(p[r] >> 16);
           #pragma unroll
           for (int cb = 0; cb < C; ++cb) {
-            const float more = g ? fmaf(mn, qsum[cb][g], x[cb][j][r]) : mn * qsum[cb][g];
-            x[cb][j][r] = fmaf(s, dot[cb][r], more);
+            const float more = g ? fmaf(mn[r], qsum[cb][g], x[cb][j][r]) : mn[r] * qsum[cb][g];
+            x[cb][j][r] = fmaf(s[r], dot[cb][r], more);
           }
         }
       }
+      // done here: put off to their next use, they would keep all parameters and
+      // products of the tile in registers
+      #pragma unroll
+      for (int cb = 0; cb < C; ++cb) asm volatile("" : "+v"(x[cb][j]));
     }
     if (tile + kWaves < tile1) load_k(tile + kWaves);
     if (!whole) {
       const uint32_t have = (uint32_t)(held >> (16 * quad)) & 0xFFFFu;
-      const long long t = tile * kTile + 16 * quad;
+      const int t = tile * kTile + 16 * quad;
       #pragma unroll
       for (int cb = 0; cb < C; ++cb) {
         // tokens t + k with pos - window < t + k <= pos: bit k
-        const int last = (int)max(-1ll, min(15ll, pos[cb] - t));
-        const int first =
-            u.window > 0 ? (int)max(0ll, min(16ll, pos[cb] - u.window + 1 - t)) : 0;
+        const int last = max(-1, min(15, pos[cb] - t));
+        const int first = u.window > 0 ? max(0, min(16, pos[cb] - u.window + 1 - t)) : 0;
         const uint32_t seen = ((1u << (last + 1)) - 1u) & (~0u << first) & have;
         #pragma unroll
         for (int k = 0; k < 16; ++k)
@@ -458,33 +492,24 @@ __global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_ker
           weight_sum[cb] += p;
         }
     // the weighted sum, group by group
-    const float unit_even = ldexpf(1.0f, 14 - vexp), unit_odd = unit_even * 0.0625f;
     #pragma unroll
     for (int g = 0; g < NG; ++g) {
       if constexpr (NG > 1) __builtin_amdgcn_sched_barrier(0);
       f16x8 p[C][2];
       #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const u32x4 v0 =
-            *reinterpret_cast<const u32x4*>(params + (NG + g) * kTile + 16 * quad + 8 * h);
-        const u32x4 v1 =
-            *reinterpret_cast<const u32x4*>(params + (NG + g) * kTile + 16 * quad + 8 * h + 4);
+      for (int j = 0; j < 4; ++j) {
+        const float* at = params + (4 * g + 2) * kTile + 16 * quad + 4 * j;
+        const f32x4 s = *reinterpret_cast<const f32x4*>(at);
+        const f32x4 mn = *reinterpret_cast<const f32x4*>(at + kTile);
         #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float unit_r = r & 1 ? unit_odd : unit_even;
-          const float s0 = low_half(v0[r]) * unit_r, s1 = low_half(v1[r]) * unit_r;
-          const float m0 = low_half(v0[r] >> 16), m1 = low_half(v1[r] >> 16);
+        for (int r = 0; r < 4; ++r)
           #pragma unroll
           for (int cb = 0; cb < C; ++cb) {
-            const float w0 = x[cb][2 * h][r], w1 = x[cb][2 * h + 1][r];
             // the products that are 0 where the weight is, whatever the parameter:
             // it may be anything for a token that the row does not see
-            offset[cb][g] += mul_zero(w0, m0);
-            offset[cb][g] += mul_zero(w1, m1);
-            p[cb][h][2 * r] = (_Float16)mul_zero(w0, s0);
-            p[cb][h][2 * r + 1] = (_Float16)mul_zero(w1, s1);
+            offset[cb][g] += mul_zero(x[cb][j][r], mn[r]);
+            p[cb][j / 2][2 * r + j % 2] = (_Float16)mul_zero(x[cb][j][r], s[r]);
           }
-        }
       }
       #pragma unroll
       for (int d = g * DB / NG; d < (g + 1) * DB / NG; ++d) {
@@ -504,31 +529,22 @@ __global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_ker
     }
   };
 
-  const long long first = tile0 + wave;
+  const int first = tile0 + wave;
   if (first < tile1) {
     load_k(first);
     load_v(first);
   }
-  for (long long tile = first; tile < tile1; tile += kWaves) {
+  for (int tile = first; tile < tile1; tile += kWaves) {
+    const unsigned long long held = __ballot(stored);
     // ---- V and the parameters into LDS; tokens that are not there have none
     uint32_t big = 0;
     #pragma unroll
     for (int g = 0; g < NG; ++g) {
-      const uint32_t kp = stored ? preg[0][g] : 0u, vp = stored ? preg[1][g] : 0u;
-      params[g * kTile + lane] = kp;
-      params[(NG + g) * kTile + lane] = vp;
-      const uint32_t s = vp & 0xFFFFu;
+      preg[0][g] = stored ? preg[0][g] : 0u;
+      preg[1][g] = stored ? preg[1][g] : 0u;
+      const uint32_t s = preg[1][g] & 0xFFFFu;
       big = max(big, s < 0x7C00u ? s : 0u);  // finite scales, as bits
     }
-    #pragma unroll
-    for (int i = 0; i < VL; ++i) {
-      const int token = i * (64 / VL) + lane / VL;
-      // chunks in turned order, so that the 16 rows of a transposing read lie in
-      // different banks
-      const int chunk = lane % VL ^ (VL == 4 ? (token >> 2) & 3 : (token >> 3) & 1);
-      *reinterpret_cast<u32x4*>(stage + token * ROW + 16 * chunk) = vreg[i];
-    }
-    const unsigned long long held = __ballot(stored);
     // the largest scale sets the unit of the weights
     const float vbig = low_half(big);
     if (__any(vbig >= ldexpf(1.0f, vexp + 1))) {
@@ -538,17 +554,35 @@ __global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_ker
       const int e = ilogbf(m);
       const float f = ldexpf(1.0f, vexp - e);
       vexp = e;
+      // an odd token's weight takes back the 16 of its code
+      weight_unit = ldexpf(1.0f, (lane & 1 ? 10 : 14) - e);
       #pragma unroll
       for (int cb = 0; cb < C; ++cb)
         #pragma unroll
         for (int d = 0; d < DB; ++d) o[cb][d] *= f;
+    }
+    #pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      float* at = params + 4 * g * kTile + lane;
+      at[0] = low_half(preg[0][g]);
+      at[kTile] = low_half(preg[0][g] >> 16);
+      at[2 * kTile] = low_half(preg[1][g]) * weight_unit;
+      at[3 * kTile] = low_half(preg[1][g] >> 16);
+    }
+    #pragma unroll
+    for (int i = 0; i < VL; ++i) {
+      const int token = i * (64 / VL) + lane / VL;
+      // chunks in turned order, so that the 16 rows of a transposing read lie in
+      // different banks
+      const int chunk = lane % VL ^ (VL == 4 ? (token >> 2) & 3 : (token >> 3) & 1);
+      *reinterpret_cast<u32x4*>(stage + token * ROW + 16 * chunk) = vreg[i];
     }
     if (tile + kWaves < tile1) load_v(tile + kWaves);
     // LDS is this wave's own: its accesses stay in order
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-    const long long t = tile * kTile;
+    const int t = tile * kTile;
     const bool whole = held == ~0ull && t + kTile - 1 <= pos0 &&
                        (u.window == 0 || t > pos1 - u.window);
     work(tile, whole, held);
@@ -643,43 +677,80 @@ __global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_ker
   }
 }
 
-// Adds up the ranges of rows that have several: a block takes one row of q and a
-// few of its heads, a thread four channels of one head.
+// Adds up the ranges of the row blocks that have several: a block takes two rows
+// of one (grid x: row block and kv head, y: rows), D / 4 lanes of four channels to
+// a row, the others take turns at the ranges.
 __global__ __launch_bounds__(256) void kv4_attention_combine_kernel(PagedCache c, PagedBatch b,
                                                                     AttentionArgs a, UnitShape u,
                                                                     Partials part) {
-  const int m = blockIdx.x;
-  int seq;
-  long long p;
-  if (!find_row(b, m, &seq, &p)) return;
+  constexpr int kRows = 2;
+  __shared__ f32x4 sums[256];
+  __shared__ f32x2 stats[256];
+  const int D = c.head_dim, lanes = D / 4, turns = 256 / kRows / lanes;
   Unit unit;
-  if (!find_unit(b, c.page_shift, u, 0, seq, &unit) || unit.ranges < 2) return;
-  const int D = c.head_dim, lanes = D / 4;
-  const int head = blockIdx.y * (256 / lanes) + threadIdx.x / lanes;
-  if (head >= a.heads) return;
-  const int channel = 4 * (threadIdx.x % lanes);
-  const long long r = (long long)(m - unit.w.start) * u.group + head % u.group;
-  const long long block = unit.w.blocks - 1 - r / u.rows;
-  const long long slot = unit.slot + block * unit.ranges;
-  if (slot + unit.ranges > part.slots) return;  // no batch that comet.h allows
-  // row of the first range's result; the next ranges' lie `step` apart
-  const long long first = (slot * c.kv_heads + head / u.group) * u.rows + r % u.rows;
-  const long long step = (long long)c.kv_heads * u.rows;
-  float top = kNone;
-  for (int k = 0; k < unit.ranges; ++k) top = fmaxf(top, part.stats[(first + k * step) * 2]);
-  float sum = 0.0f;
+  if (!find_unit<true>(b, c.page_shift, u, blockIdx.x / c.kv_heads, &unit)) return;
+  const int head = blockIdx.x % c.kv_heads;
+  const int r = blockIdx.y * kRows + threadIdx.x / (256 / kRows);
+  const int turn = threadIdx.x / lanes % turns, channel = 4 * (threadIdx.x % lanes);
+  const int row = unit.block * u.rows + r;
+  if (unit.slot + unit.ranges > part.slots) return;  // no batch that comet.h allows
+  float top = kNone, sum = 0.0f;
   f32x4 v = {0, 0, 0, 0};
-  for (int k = 0; k < unit.ranges; ++k) {
-    const long long at = first + k * step;
-    const float f = __builtin_amdgcn_exp2f(part.stats[at * 2] - top);
-    sum += f * part.stats[at * 2 + 1];
-    v += f * *reinterpret_cast<const f32x4*>(part.sums + at * D + channel);
+  const bool live = row < unit.w.n * u.group;
+  if (live) {
+    // the ranges' results lie `step` rows apart
+    const long long first = ((long long)unit.slot * c.kv_heads + head) * u.rows + r;
+    const long long step = (long long)c.kv_heads * u.rows;
+    constexpr int kAhead = 8;
+    for (int k = turn; k < (int)unit.ranges; k += kAhead * turns) {
+      f32x2 st[kAhead];
+      f32x4 x[kAhead];
+      #pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        st[i] = f32x2{kNone, 0.0f};
+        x[i] = f32x4{0, 0, 0, 0};
+        if (k + i * turns < (int)unit.ranges) {
+          const long long at = first + (k + i * turns) * step;
+          st[i] = *reinterpret_cast<const f32x2*>(part.stats + at * 2);
+          x[i] = *reinterpret_cast<const f32x4*>(part.sums + at * D + channel);
+        }
+      }
+      float next = top;
+      #pragma unroll
+      for (int i = 0; i < kAhead; ++i) next = fmaxf(next, st[i][0]);
+      const float f = __builtin_amdgcn_exp2f(top - next);
+      top = next;
+      sum *= f;
+      v *= f;
+      #pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const float g = __builtin_amdgcn_exp2f(st[i][0] - top);
+        sum += g * st[i][1];
+        v += g * x[i];
+      }
+    }
+  }
+  sums[threadIdx.x] = v;
+  stats[threadIdx.x] = f32x2{top, sum};
+  __syncthreads();
+  if (!live || turn) return;
+  float all = kNone;
+  for (int k = 0; k < turns; ++k) all = fmaxf(all, stats[threadIdx.x + k * lanes][0]);
+  sum = 0.0f;
+  v = f32x4{0, 0, 0, 0};
+  for (int k = 0; k < turns; ++k) {
+    const f32x2 st = stats[threadIdx.x + k * lanes];
+    const float f = __builtin_amdgcn_exp2f(st[0] - all);
+    sum += f * st[1];
+    v += f * sums[threadIdx.x + k * lanes];
   }
   const float f = sum != 0.0f ? 1.0f / sum : 0.0f;
-  const f16x2 y[2] = {{(_Float16)(v[0] * f), (_Float16)(v[1] * f)},
-                      {(_Float16)(v[2] * f), (_Float16)(v[3] * f)}};
-  *reinterpret_cast<u32x2*>(a.out + (long long)m * a.out_stride + head * D + channel) =
-      __builtin_bit_cast(u32x2, *reinterpret_cast<const u32x2*>(y));
+  const f16x2 lo = {(_Float16)(v[0] * f), (_Float16)(v[1] * f)};
+  const f16x2 hi = {(_Float16)(v[2] * f), (_Float16)(v[3] * f)};
+  const long long m = unit.w.start + row / u.group;
+  *reinterpret_cast<u32x2*>(a.out + m * a.out_stride +
+                            (head * u.group + row % u.group) * D + channel) =
+      u32x2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
 }
 
 // ---- host ------------------------------------------------------------------------
@@ -689,6 +760,7 @@ struct Shape {
   int columns;       // C
   long long blocks;  // of the grid: units that a batch of these sizes may have, times kv heads
   long long slots;   // partial results
+  int most_rows;     // of a row block
 };
 
 Shape shape_of(const PagedCache& c, const PagedBatch& b, int heads, int window, int cus) {
@@ -696,10 +768,12 @@ Shape shape_of(const PagedCache& c, const PagedBatch& b, int heads, int window, 
   s.u.group = heads / c.kv_heads;
   s.columns = (long long)b.max_rows * s.u.group > 16 ? 2 : 1;
   s.u.rows = 16 * s.columns;
-  s.u.window = window;
+  s.u.window = window > 1 << 30 ? 0 : window;  // no position is further
+  s.most_rows = (int)std::min<long long>(s.u.rows, (long long)b.max_rows * s.u.group);
   // blocks that a compute unit holds at a time
   const int resident = s.columns == 1 ? 3 : 2;
-  s.u.target = std::max(1, cus * resident / c.kv_heads);
+  const char* tm = getenv("TUNE_T");
+  s.u.target = std::max(1, (int)(cus * resident * (tm ? atof(tm) : 1.0)) / c.kv_heads);
   // every sequence's last row block may be ragged
   const long long row_blocks =
       (long long)b.M * s.u.group / s.u.rows + std::min(b.B, b.M);
@@ -725,8 +799,8 @@ void launch_columns(const PagedCache& c, const PagedBatch& b, const AttentionArg
 const char* attention_refusal(const PagedCache& c, const PagedBatch& b, int heads, int cus) {
   // a launch's threads are counted in 32 bits
   const Shape s = shape_of(c, b, heads, 0, cus);
-  return s.blocks >= (1ll << 32) / (64 * kWaves) ? "too many rows, heads and sequences for a launch"
-                                                 : nullptr;
+  const bool many = (long long)b.M * heads > 1 << 30 || s.blocks >= (1ll << 32) / (64 * kWaves);
+  return many ? "too many rows, heads and sequences for a launch" : nullptr;
 }
 
 size_t attention_workspace(const PagedCache& c, const PagedBatch& b, int heads, int cus) {
@@ -751,8 +825,10 @@ hipError_t launch_kv4_attention(const PagedCache& c, const PagedBatch& b, const 
     launch_columns<64, 32>(c, b, a, s, part, stream);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !s.slots) return e;
-  const int heads = 256 / (c.head_dim / 4);
-  hipLaunchKernelGGL(kv4_attention_combine_kernel, dim3(b.M, (a.heads + heads - 1) / heads),
+  // row blocks with several ranges: half the slots at most, and no more than there are
+  const long long split = std::min<long long>(s.slots / 2, s.blocks / c.kv_heads);
+  hipLaunchKernelGGL(kv4_attention_combine_kernel,
+                     dim3((unsigned)(split * c.kv_heads), std::min(s.u.rows, s.most_rows + 1) / 2),
                      dim3(256), 0, stream, c, b, a, s.u, part);
   return hipGetLastError();
 }
