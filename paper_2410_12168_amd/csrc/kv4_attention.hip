@@ -24,9 +24,10 @@
 //   - V's operand needs 8 tokens of a channel in a lane; the cache has channels
 //     in a row.  The transposing LDS read (ds_read_b64_tr_b4: 16 rows of 16
 //     nibbles) turns 16 tokens x 16 channels at a time.
-//   - token 16 h + 4 j + r of a 64-token tile is row 4 h + r of the j-th score
-//     product, so a lane's scores are those of the tokens that its lanes of V's
-//     operand hold: the weights go from one product into the other in place.
+//   - token 16 j + 4 h + r of a 64-token tile is row 4 h + r of the j-th score
+//     product, and V's rows are read in the order that gives quad h of the lanes
+//     the tokens whose scores it has: the weights go from one product into the
+//     other in place.
 //
 // Work decomposition: a block of four waves takes one (sequence, kv head, 16 C
 // rows of its q heads, range of tokens); the waves take turns at its 64-token
@@ -351,57 +352,80 @@ __global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_ker
   uint8_t* stage = lds + wave * STAGE;
   float* params = reinterpret_cast<float*>(stage + kTile * ROW);
 
+  // ---- pages: lane 4 i + k has the one of granule k (16 tokens) of this wave's i-th
+  // next tile, or -1, so that a tile's pages are scalars and its loads do not wait
+  // behind a load of the table
+  const int32_t* table = b.block_table + (long long)unit.seq * b.max_pages;
+  int pages = -1;
+  auto load_pages = [&](int tile) {
+    const int token = (tile + (lane >> 2) * kWaves) * kTile + 16 * (lane & 3);
+    const int i = token >> c.page_shift;
+    const int page = i < b.max_pages ? table[i] : -1;
+    pages = (unsigned)page < (unsigned)c.num_pages ? page : -1;
+  };
+  auto page_of = [&](int i, int k) { return __builtin_amdgcn_readlane(pages, 4 * i + k); };
+  // first row of granule k's 16 in the cache; a hole reads page 0
+  auto granule_row = [&](int tile, int i, int k) -> long long {
+    return cache_row(c, max(page_of(i, k), 0), head, tile * kTile + 16 * k);
+  };
+
   // ---- loads of a tile: into registers, a tile ahead
   uint32_t kreg[4][KS];
   u32x4 vreg[VL];
   uint32_t preg[2][NG];
-  bool stored;  // this lane's token (for the parameters) is in the cache
-  const int32_t* table = b.block_table + (long long)unit.seq * b.max_pages;
-
-  auto page_at = [&](int token) -> int {  // of a 16-token granule
-    const int i = token >> c.page_shift;
-    if (i >= b.max_pages) return -1;
-    const int page = table[i];
-    return (unsigned)page < (unsigned)c.num_pages ? page : -1;
-  };
-  // first row of the granule's 16 in the cache; a hole reads page 0
-  auto granule_row = [&](int page, int token) -> long long {
-    return cache_row(c, max(page, 0), head, token);
-  };
-  auto load_k = [&](int tile) {
-    const int t = tile * kTile + 16 * (col >> 2);  // the granule of K's row `col`
-    const uint8_t* at = c.k_codes + (granule_row(page_at(t), t) + (col & 3)) * ROW + ROW / 4 * quad;
+  unsigned long long held = 0;  // tokens that are in the cache
+  auto load_k = [&](int tile, int ahead) {
     #pragma unroll
     for (int j = 0; j < 4; ++j) {
+      const uint8_t* at =
+          c.k_codes + granule_row(tile, ahead, j) * ROW + (unsigned)(col * ROW + ROW / 4 * quad);
       if constexpr (KS == 4) {
-        const u32x4 v = *reinterpret_cast<const u32x4*>(at + 4 * j * ROW);
+        const u32x4 v = *reinterpret_cast<const u32x4*>(at);
         kreg[j][0] = v[0], kreg[j][1] = v[1], kreg[j][2] = v[2], kreg[j][3] = v[3];
       } else {
-        const u32x2 v = *reinterpret_cast<const u32x2*>(at + 4 * j * ROW);
+        const u32x2 v = *reinterpret_cast<const u32x2*>(at);
         kreg[j][0] = v[0], kreg[j][1] = v[1];
       }
     }
   };
-  auto load_v = [&](int tile) {
-    const int t = tile * kTile;
+  auto load_v = [&](int tile, int ahead) {
+    long long rows4[4];
+    #pragma unroll
+    for (int k = 0; k < 4; ++k) rows4[k] = granule_row(tile, ahead, k);
     #pragma unroll
     for (int i = 0; i < VL; ++i) {
-      const int token = i * (64 / VL) + lane / VL, tv = t + (token & ~15);
-      const long long row = granule_row(page_at(tv), tv) + (token & 15);
-      vreg[i] = *reinterpret_cast<const u32x4*>(c.v_codes + row * ROW + 16 * (lane % VL));
+      if constexpr (VL == 4) {
+        vreg[i] = *reinterpret_cast<const u32x4*>(c.v_codes + rows4[i] * ROW + 16u * lane);
+      } else {
+        const long long row = lane < 32 ? rows4[2 * i] : rows4[2 * i + 1];
+        vreg[i] = *reinterpret_cast<const u32x4*>(c.v_codes + row * ROW + 16u * (lane & 31));
+      }
     }
-    const int tp = t + 16 * quad, page = page_at(tp);
-    const long long row = granule_row(page, tp) + col;
-    stored = page >= 0 && t + lane < w.len;
+    const long long mine = quad < 2 ? (quad == 0 ? rows4[0] : rows4[1])
+                                    : (quad == 2 ? rows4[2] : rows4[3]);
+    const long long at = (mine + col) * NG;
     #pragma unroll
     for (int g = 0; g < NG; ++g) {
-      preg[0][g] = reinterpret_cast<const uint32_t*>(c.k_params)[row * NG + g];
-      preg[1][g] = reinterpret_cast<const uint32_t*>(c.v_params)[row * NG + g];
+      preg[0][g] = reinterpret_cast<const uint32_t*>(c.k_params)[at + g];
+      preg[1][g] = reinterpret_cast<const uint32_t*>(c.v_params)[at + g];
     }
+    held = 0;
+    #pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (page_of(ahead, k) >= 0) held |= 0xFFFFull << (16 * k);
+    const int left = w.len - tile * kTile;
+    if (left < kTile) held &= (1ull << max(left, 0)) - 1;
+  };
+
+  // Where a 16-byte chunk of V's row lies in LDS: the 16 rows of a transposing read
+  // (16 j + 4 quad + r, one chunk) in different banks.
+  auto v_place = [](int token, int chunk) {
+    if constexpr (VL == 4) return token * ROW + 16 * (chunk ^ token >> 4);
+    return (token ^ token >> 5 << 2) * ROW + 16 * (chunk ^ (token >> 4 & 1));
   };
 
   // ---- one tile
-  auto work = [&](int tile, bool whole, unsigned long long held) {
+  auto work = [&](int tile, bool whole, unsigned long long have, int ahead) {
     f32x4 x[C][4];
     #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -426,7 +450,7 @@ __global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_ker
             dot[cb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[cb][s], dot[cb], 0, 0, 0);
         }
         if constexpr (NG > 1) __builtin_amdgcn_sched_barrier(0);  // keeps registers few
-        const float* at = params + 4 * g * kTile + 16 * quad + 4 * j;
+        const float* at = params + 4 * g * kTile + 16 * j + 4 * quad;
         const f32x4 s = *reinterpret_cast<const f32x4*>(at);
         const f32x4 mn = *reinterpret_cast<const f32x4*>(at + kTile);
         #pragma unroll
@@ -443,19 +467,23 @@ __global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_ker
       #pragma unroll
       for (int cb = 0; cb < C; ++cb) asm volatile("" : "+v"(x[cb][j]));
     }
-    if (tile + kWaves < tile1) load_k(tile + kWaves);
+    if (tile + kWaves < tile1) load_k(tile + kWaves, ahead);
     if (!whole) {
-      const uint32_t have = (uint32_t)(held >> (16 * quad)) & 0xFFFFu;
-      const int t = tile * kTile + 16 * quad;
+      const int t = tile * kTile;
       #pragma unroll
       for (int cb = 0; cb < C; ++cb) {
         // tokens t + k with pos - window < t + k <= pos: bit k
-        const int last = max(-1, min(15, pos[cb] - t));
-        const int first = u.window > 0 ? max(0, min(16, pos[cb] - u.window + 1 - t)) : 0;
-        const uint32_t seen = ((1u << (last + 1)) - 1u) & (~0u << first) & have;
+        const int last = max(-1, min(kTile - 1, pos[cb] - t));
+        const int first = u.window > 0 ? max(0, min(kTile, pos[cb] - u.window + 1 - t)) : 0;
+        unsigned long long seen = have;
+        seen = last < kTile - 1 ? seen & ((1ull << (last + 1)) - 1) : seen;
+        seen = first < kTile ? seen >> first << first : 0;
+        seen >>= 4 * quad;  // bit 16 j + r
         #pragma unroll
-        for (int k = 0; k < 16; ++k)
-          if (!(seen >> k & 1u)) x[cb][k / 4][k % 4] = -INFINITY;
+        for (int k = 0; k < 16; ++k) {
+          const uint32_t half = (uint32_t)(seen >> (k < 8 ? 0 : 32));
+          if (!(half >> (16 * (k / 4 % 2) + k % 4) & 1u)) x[cb][k / 4][k % 4] = -INFINITY;
+        }
       }
     }
     // running maximum; what was added up before shrinks with it
@@ -498,7 +526,7 @@ __global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_ker
       f16x8 p[C][2];
       #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float* at = params + (4 * g + 2) * kTile + 16 * quad + 4 * j;
+        const float* at = params + (4 * g + 2) * kTile + 16 * j + 4 * quad;
         const f32x4 s = *reinterpret_cast<const f32x4*>(at);
         const f32x4 mn = *reinterpret_cast<const f32x4*>(at + kTile);
         #pragma unroll
@@ -513,9 +541,9 @@ __global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_ker
       }
       #pragma unroll
       for (int d = g * DB / NG; d < (g + 1) * DB / NG; ++d) {
-        // 16-byte chunk d / 2 of token row 16 quad + col, where the store put it
-        const int chunk = VL == 4 ? (d / 2) ^ (col >> 2) : (d / 2) ^ (col >> 3);
-        const uint8_t* at = stage + (16 * quad + col) * ROW + 16 * chunk + 8 * (d & 1);
+        // 16-byte chunk d / 2 of this lane's row, where the store put it
+        const uint8_t* at =
+            stage + v_place(16 * (col >> 2) + 4 * quad + (col & 3), d / 2) + 8 * (d & 1);
         const i32x2 v = __builtin_amdgcn_ds_read_tr4_b64_v2i32(
             (__attribute__((address_space(3))) i32x2*)at);
         #pragma unroll
@@ -530,12 +558,15 @@ __global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_ker
   };
 
   const int first = tile0 + wave;
+  int ahead = 0;  // where in `pages` the next tile is
   if (first < tile1) {
-    load_k(first);
-    load_v(first);
+    load_pages(first);
+    load_k(first, 0);
+    load_v(first, 0);
   }
   for (int tile = first; tile < tile1; tile += kWaves) {
-    const unsigned long long held = __ballot(stored);
+    const unsigned long long have = held;
+    const bool stored = have >> lane & 1;
     // ---- V and the parameters into LDS; tokens that are not there have none
     uint32_t big = 0;
     #pragma unroll
@@ -572,20 +603,23 @@ __global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_ker
     #pragma unroll
     for (int i = 0; i < VL; ++i) {
       const int token = i * (64 / VL) + lane / VL;
-      // chunks in turned order, so that the 16 rows of a transposing read lie in
-      // different banks
-      const int chunk = lane % VL ^ (VL == 4 ? (token >> 2) & 3 : (token >> 3) & 1);
-      *reinterpret_cast<u32x4*>(stage + token * ROW + 16 * chunk) = vreg[i];
+      *reinterpret_cast<u32x4*>(stage + v_place(token, lane % VL)) = vreg[i];
     }
-    if (tile + kWaves < tile1) load_v(tile + kWaves);
+    if (tile + kWaves < tile1) {
+      if (++ahead == 16) {
+        load_pages(tile + kWaves);
+        ahead = 0;
+      }
+      load_v(tile + kWaves, ahead);
+    }
     // LDS is this wave's own: its accesses stay in order
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
     const int t = tile * kTile;
-    const bool whole = held == ~0ull && t + kTile - 1 <= pos0 &&
+    const bool whole = have == ~0ull && t + kTile - 1 <= pos0 &&
                        (u.window == 0 || t > pos1 - u.window);
-    work(tile, whole, held);
+    work(tile, whole, have, ahead);
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
