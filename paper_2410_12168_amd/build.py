@@ -24,7 +24,7 @@ LIB = os.path.join(HERE, "libcomet.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 SOURCES = ["quantize.hip", "gemm.hip", "gemm_skinny.hip", "kv4.hip", "noalloc.hip", "rope.hip",
-           "kv4_cache.hip", "kv4_attention.hip", "scheduler.cpp", "calib.cpp", "comet_api.cpp"]
+           "kv4_cache.hip", "kv4_attention.hip", "kv4_attention_many.hip", "scheduler.cpp", "calib.cpp", "comet_api.cpp"]
 
 # The GEMM's inner loop interleaves MFMAs with the dequantization FMAs: keep
 # MFMA results in VGPRs (no accumulator-register copies).

@@ -35,217 +35,18 @@
 // on the device (find_unit): every block of every sequence gets about the same
 // number of tiles, about `target` ranges in all, and a second kernel adds up the
 // ranges of a sequence that has more than one.
-#include <hip/hip_fp16.h>
-#include <hip/hip_runtime.h>
-#include <stdint.h>
-
 #include <algorithm>
 
-#include "paged.h"
+#include "attention.h"
 
 namespace comet {
 
 namespace {
 
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef int i32x2 __attribute__((ext_vector_type(2)));
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-
-constexpr float kLog2e = 1.44269504088896340736f;
-constexpr float kNone = -1e30f;  // maximum of no scores
-constexpr int kTile = 64;        // tokens a wave takes at a time
-constexpr int kWaves = 4;
-// fewest tiles in a range: one for each wave
-constexpr int kMinTiles = kWaves;
-
-__device__ inline float low_half(uint32_t w) {
-  return __half2float(__ushort_as_half((unsigned short)w));
-}
-
-// Rows of 16 lanes: the odd rows of a change places with the even rows of b
-// (swap16), or a's upper half with b's lower (swap32).
-__device__ inline void swap16(uint32_t& a, uint32_t& b) {
-  const auto r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
-  a = r[0];
-  b = r[1];
-}
-__device__ inline void swap32(uint32_t& a, uint32_t& b) {
-  const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
-  a = r[0];
-  b = r[1];
-}
-
-// Maximum and sum over the four lanes of a column (l, l ^ 16, l ^ 32, l ^ 48).
-template <typename F>
-__device__ inline float over_quads(float v, F f) {
-  uint32_t a = __float_as_uint(v), b = a;
-  swap16(a, b);
-  v = f(__uint_as_float(a), __uint_as_float(b));
-  a = b = __float_as_uint(v);
-  swap32(a, b);
-  return f(__uint_as_float(a), __uint_as_float(b));
-}
-__device__ inline float quad_max(float v) {
-  return over_quads(v, [](float a, float b) { return fmaxf(a, b); });
-}
-__device__ inline float quad_sum(float v) {
-  return over_quads(v, [](float a, float b) { return a + b; });
-}
-
-// Sums over the lanes up to each (the last lane has all 64), without LDS: shifts
-// within rows of 16, then the last lanes of rows 0 and 2, then of row 1.
-template <int CTRL, int ROWS, typename T>
-__device__ inline T shifted(T v) {
-  return __builtin_bit_cast(
-      T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, ROWS, 0xF, ROWS == 0xF));
-}
-template <typename T>
-__device__ inline T sum_upto(T v) {
-  v += shifted<0x111, 0xF>(v);
-  v += shifted<0x112, 0xF>(v);
-  v += shifted<0x114, 0xF>(v);
-  v += shifted<0x118, 0xF>(v);
-  v += shifted<0x142, 0xA>(v);
-  v += shifted<0x143, 0xC>(v);
-  return v;
-}
-
-// a * b, and 0 where either is 0 whatever the other is (v_mul_legacy_f32).
-extern "C" __device__ float mul_zero(float a, float b) __asm("llvm.amdgcn.fmul.legacy");
-
-// Eight codes as fp16, order (0, 4, 1, 5, 2, 6, 3, 7), times 2^-24 and, for the
-// odd ones, 2^-20.
-__device__ inline f16x8 codes_f16(uint32_t x) {
-  const u32x4 r = {x & 0x000F000Fu, x & 0x00F000F0u, (x >> 8) & 0x000F000Fu,
-                   (x >> 8) & 0x00F000F0u};
-  return __builtin_bit_cast(f16x8, r);
-}
-
-// ---- which part of the work ------------------------------------------------
-
-struct UnitShape {
-  int group;     // q heads per kv head
-  int rows;      // q rows (of all heads of a group) per block
-  int window;
-  int target;    // token ranges to aim at, per kv head
-};
-
-struct SeqWork {
-  int start, n;    // first row, rows
-  int len;         // tokens
-  uint32_t blocks; // row blocks
-  uint32_t first;  // first tile that any row sees
-  uint32_t tiles;  // tiles from there on (1 at least)
-};
-
-__device__ inline SeqWork seq_work(const PagedBatch& b, int page_shift, const UnitShape& u,
-                                   int seq) {
-  SeqWork w{0, 0, 0, 0, 0, 0};
-  if (seq >= b.B) return w;
-  w.start = max(0, min(b.M, b.row_start[seq]));
-  w.n = max(0, max(0, min(b.M, b.row_start[seq + 1])) - w.start);
-  w.len = max(-b.M, min(1 << 30, b.seq_lens[seq]));
-  const int seen = max(0, min(w.len, b.max_pages << page_shift));  // 2^30 at most
-  const int low = w.len - w.n - u.window + 1;                       // of the first row's window
-  w.blocks = ((uint32_t)w.n * u.group + u.rows - 1) / u.rows;
-  w.first = u.window > 0 ? max(0, low) / kTile : 0;
-  w.tiles = max(1, (seen + kTile - 1) / kTile - (int)w.first);
-  return w;
-}
-
-// One block's work: row block `block` of sequence `seq`, range `range` of
-// `ranges`, in which the sequence's tiles are shared out evenly.
-struct Unit {
-  int seq;
-  uint32_t block, range, ranges;
-  uint32_t slot;  // of the partial result
-  SeqWork w;
-};
-
-// Lane `at`'s value (`at` the same in all lanes) where the compiler knows that all
-// lanes have it.
-template <typename T>
-__device__ inline T from_lane(T v, int at) {
-  return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), at));
-}
-
-// Tiles of a range at most, from the work of all sequences: the same in every wave
-// of a launch.  Rounded up by more than the 32-bit sum can be off, so that the
-// ranges of full length are `target` at most.
-__device__ inline float tiles_per_range(const PagedBatch& b, int page_shift, const UnitShape& u) {
-  const int lane = threadIdx.x & 63;
-  float total = 0.0f;
-  for (int s = 0; s < b.B; s += 64) {
-    const SeqWork w = seq_work(b, page_shift, u, s + lane);
-    total += (float)w.blocks * (float)w.tiles;
-  }
-  total = from_lane(sum_upto(total), 63) * 1.001f;
-  return fmaxf((float)kMinTiles, ceilf(total / (float)u.target));
-}
-
-__device__ inline uint32_t ranges_of(const SeqWork& w, float per) {
-  return (uint32_t)ceilf((float)w.tiles / per);
-}
-
-// Unit `index`, counted over sequences, row blocks and ranges (SPLIT: row block
-// `index` of those whose sequence has more than one range).  False if there is
-// none.  Sums of 32 bits: more than a launch can have only in batches that the
-// interface does not allow, whose units are then any or none of the batch's.
-template <bool SPLIT>
-__device__ inline bool find_unit(const PagedBatch& b, int page_shift, const UnitShape& u,
-                                 uint32_t index, Unit* out) {
-  const int lane = threadIdx.x & 63;
-  const float per = tiles_per_range(b, page_shift, u);
-  uint32_t before = 0, slots_before = 0;
-  for (int s = 0; s < b.B; s += 64) {
-    const SeqWork w = seq_work(b, page_shift, u, s + lane);
-    const uint32_t ranges = ranges_of(w, per);
-    const uint32_t slots = ranges > 1 ? w.blocks * ranges : 0;
-    const uint32_t mine = SPLIT ? (ranges > 1 ? w.blocks : 0) : w.blocks * ranges;
-    const uint32_t upto = before + sum_upto(mine), slots_upto = slots_before + sum_upto(slots);
-    const unsigned long long hit = __ballot(mine > 0 && upto > index);
-    if (hit) {
-      const int at = __builtin_amdgcn_readfirstlane(__ffsll((long long)hit) - 1);
-      const uint32_t k = index - from_lane(upto - mine, at);
-      out->seq = s + at;
-      out->ranges = from_lane(ranges, at);
-      out->w.start = from_lane(w.start, at);
-      out->w.n = from_lane(w.n, at);
-      out->w.len = from_lane(w.len, at);
-      out->w.blocks = from_lane(w.blocks, at);
-      out->w.first = from_lane(w.first, at);
-      out->w.tiles = from_lane(w.tiles, at);
-      const uint32_t block = SPLIT ? k : k / out->ranges;
-      out->range = SPLIT ? 0 : k % out->ranges;
-      out->slot = from_lane(slots_upto - slots, at) + block * out->ranges + out->range;
-      // the last row blocks see the most tokens: they come first
-      out->block = out->w.blocks - 1 - block;
-      return true;
-    }
-    before = from_lane(upto, 63);
-    slots_before = from_lane(slots_upto, 63);
-  }
-  return false;
-}
-
-// Partial results in the workspace: [slot][kv head][rows][D] sums and
-// [slot][kv head][rows][2] {maximum (log2), sum of weights}.  A sequence with more
-// than one range has more tiles than the longest range may have, which is at
-// least all tiles over `target`: there are fewer than 2 * target slots.
-struct Partials {
-  float* sums;
-  float* stats;
-  uint32_t slots;
-};
-
 // ---- the products --------------------------------------------------------------
 
 template <int D, int G, int C>
-__global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_kernel(
+__global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_few_kernel(
     PagedCache c, PagedBatch b, AttentionArgs a, UnitShape u, Partials part) {
   constexpr int NG = D / G;         // groups of a head
   constexpr int KS = D / 32;        // steps of the score product
@@ -472,12 +273,7 @@ __global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_ker
       const int t = tile * kTile;
       #pragma unroll
       for (int cb = 0; cb < C; ++cb) {
-        // tokens t + k with pos - window < t + k <= pos: bit k
-        const int last = max(-1, min(kTile - 1, pos[cb] - t));
-        const int first = u.window > 0 ? max(0, min(kTile, pos[cb] - u.window + 1 - t)) : 0;
-        unsigned long long seen = have;
-        seen = last < kTile - 1 ? seen & ((1ull << (last + 1)) - 1) : seen;
-        seen = first < kTile ? seen >> first << first : 0;
+        unsigned long long seen = seen_tokens(pos[cb], t, u.window, have);
         seen >>= 4 * quad;  // bit 16 j + r
         #pragma unroll
         for (int k = 0; k < 16; ++k) {
@@ -533,10 +329,8 @@ __global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_ker
         for (int r = 0; r < 4; ++r)
           #pragma unroll
           for (int cb = 0; cb < C; ++cb) {
-            // the products that are 0 where the weight is, whatever the parameter:
-            // it may be anything for a token that the row does not see
-            offset[cb][g] += mul_zero(x[cb][j][r], mn[r]);
-            p[cb][j / 2][2 * r + j % 2] = (_Float16)mul_zero(x[cb][j][r], s[r]);
+            offset[cb][g] = fmaf(x[cb][j][r], mn[r], offset[cb][g]);
+            p[cb][j / 2][2 * r + j % 2] = (_Float16)(x[cb][j][r] * s[r]);
           }
       }
       #pragma unroll
@@ -567,14 +361,28 @@ __global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_ker
   for (int tile = first; tile < tile1; tile += kWaves) {
     const unsigned long long have = held;
     const bool stored = have >> lane & 1;
+    bool bad = false;
     // ---- V and the parameters into LDS; tokens that are not there have none
-    uint32_t big = 0;
+    uint32_t big = 0;  // scale of V, as bits
     #pragma unroll
     for (int g = 0; g < NG; ++g) {
       preg[0][g] = stored ? preg[0][g] : 0u;
       preg[1][g] = stored ? preg[1][g] : 0u;
-      const uint32_t s = preg[1][g] & 0xFFFFu;
-      big = max(big, s < 0x7C00u ? s : 0u);  // finite scales, as bits
+      bad |= not_finite(preg[0][g]) || not_finite(preg[1][g]);
+    }
+    // tokens that are not finite make the rows that see them not-a-number, and no
+    // others: they count as zeros in the products
+    const unsigned long long poison = __ballot(bad);
+    if (poison) {
+      #pragma unroll
+      for (int cb = 0; cb < C; ++cb)
+        if (seen_tokens(pos[cb], tile * kTile, u.window, poison)) weight_sum[cb] = NAN;
+    }
+    #pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      preg[0][g] = bad ? 0u : preg[0][g];
+      preg[1][g] = bad ? 0u : preg[1][g];
+      big = max(big, preg[1][g] & 0xFFFFu);
     }
     // the largest scale sets the unit of the weights
     const float vbig = low_half(big);
@@ -711,121 +519,184 @@ __global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_ker
   }
 }
 
-// Adds up the ranges of the row blocks that have several: a block takes two rows
-// of one (grid x: row block and kv head, y: rows), D / 4 lanes of four channels to
-// a row, the others take turns at the ranges.
+// Adds up the ranges of the row blocks that have several: a block takes some rows of
+// one (grid x: row block and kv head, y: rows).  D / 4 lanes of four channels make a
+// group; a group takes a row, or, the more ranges there are, several take turns at
+// those of one.
+constexpr int kCombineRows = 4;       // of a block, in the kernel for few rows
+constexpr int kCombineManyRows = 32;  // in the other
+constexpr int kAhead = 8;             // ranges that a group has in flight
+
 __global__ __launch_bounds__(256) void kv4_attention_combine_kernel(PagedCache c, PagedBatch b,
-                                                                    AttentionArgs a, UnitShape u,
-                                                                    Partials part) {
-  constexpr int kRows = 2;
+                                                                    AttentionArgs a,
+                                                                    UnitShape few, Partials few_part,
+                                                                    UnitShape many,
+                                                                    Partials many_part,
+                                                                    int few_blocks) {
   __shared__ f32x4 sums[256];
   __shared__ f32x2 stats[256];
-  const int D = c.head_dim, lanes = D / 4, turns = 256 / kRows / lanes;
+  const bool is_few = (int)blockIdx.x < few_blocks;
+  const UnitShape u = is_few ? few : many;
+  const Partials part = is_few ? few_part : many_part;
+  const int index = blockIdx.x - (is_few ? 0 : few_blocks);
+  const int my_rows = is_few ? kCombineRows : kCombineManyRows;
+  if ((int)blockIdx.y * my_rows >= u.rows) return;
   Unit unit;
-  if (!find_unit<true>(b, c.page_shift, u, blockIdx.x / c.kv_heads, &unit)) return;
-  const int head = blockIdx.x % c.kv_heads;
-  const int r = blockIdx.y * kRows + threadIdx.x / (256 / kRows);
-  const int turn = threadIdx.x / lanes % turns, channel = 4 * (threadIdx.x % lanes);
-  const int row = unit.block * u.rows + r;
+  if (!find_unit<true>(b, c.page_shift, u, index / c.kv_heads, &unit)) return;
   if (unit.slot + unit.ranges > part.slots) return;  // no batch that comet.h allows
-  float top = kNone, sum = 0.0f;
-  f32x4 v = {0, 0, 0, 0};
-  const bool live = row < unit.w.n * u.group;
-  if (live) {
-    // the ranges' results lie `step` rows apart
-    const long long first = ((long long)unit.slot * c.kv_heads + head) * u.rows + r;
-    const long long step = (long long)c.kv_heads * u.rows;
-    constexpr int kAhead = 8;
-    for (int k = turn; k < (int)unit.ranges; k += kAhead * turns) {
-      f32x2 st[kAhead];
-      f32x4 x[kAhead];
-      #pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        st[i] = f32x2{kNone, 0.0f};
-        x[i] = f32x4{0, 0, 0, 0};
-        if (k + i * turns < (int)unit.ranges) {
-          const long long at = first + (k + i * turns) * step;
-          st[i] = *reinterpret_cast<const f32x2*>(part.stats + at * 2);
-          x[i] = *reinterpret_cast<const f32x4*>(part.sums + at * D + channel);
+  const int head = index % c.kv_heads;
+  const int D = c.head_dim, lanes = D / 4, groups = 256 / lanes;
+  int turns = 1;
+  while (turns < groups && turns * kAhead < (int)unit.ranges) turns *= 2;
+  const int group = threadIdx.x / lanes, channel = 4 * (threadIdx.x % lanes);
+  const int turn = group % turns, at_once = groups / turns;
+  const int row0 = unit.block * u.rows + blockIdx.y * my_rows;
+  const int rows = min(my_rows, unit.w.n * u.group - row0);
+  for (int r0 = 0; r0 < rows; r0 += at_once) {
+    const int r = r0 + group / turns, row = row0 + r;
+    const bool live = r < rows;
+    float top = kNone, sum = 0.0f;
+    f32x4 v = {0, 0, 0, 0};
+    if (live) {
+      // the ranges' results lie `step` rows apart
+      const long long first =
+          ((long long)unit.slot * c.kv_heads + head) * u.rows + blockIdx.y * my_rows + r;
+      const long long step = (long long)c.kv_heads * u.rows;
+      for (int k = turn; k < (int)unit.ranges; k += kAhead * turns) {
+        f32x2 st[kAhead];
+        f32x4 x[kAhead];
+        #pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+          st[i] = f32x2{kNone, 0.0f};
+          x[i] = f32x4{0, 0, 0, 0};
+          if (k + i * turns < (int)unit.ranges) {
+            const long long at = first + (k + i * turns) * step;
+            st[i] = *reinterpret_cast<const f32x2*>(part.stats + at * 2);
+            x[i] = *reinterpret_cast<const f32x4*>(part.sums + at * D + channel);
+          }
+        }
+        float next = top;
+        #pragma unroll
+        for (int i = 0; i < kAhead; ++i) next = fmaxf(next, st[i][0]);
+        const float f = __builtin_amdgcn_exp2f(top - next);
+        top = next;
+        sum *= f;
+        v *= f;
+        #pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+          const float g = __builtin_amdgcn_exp2f(st[i][0] - top);
+          sum += g * st[i][1];
+          v += g * x[i];
         }
       }
-      float next = top;
-      #pragma unroll
-      for (int i = 0; i < kAhead; ++i) next = fmaxf(next, st[i][0]);
-      const float f = __builtin_amdgcn_exp2f(top - next);
-      top = next;
-      sum *= f;
-      v *= f;
-      #pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        const float g = __builtin_amdgcn_exp2f(st[i][0] - top);
-        sum += g * st[i][1];
-        v += g * x[i];
+    }
+    if (turns > 1) {
+      __syncthreads();
+      sums[threadIdx.x] = v;
+      stats[threadIdx.x] = f32x2{top, sum};
+      __syncthreads();
+      float all = kNone;
+      for (int k = 0; k < turns; ++k)
+        all = fmaxf(all, stats[threadIdx.x + (k - turn) * lanes][0]);
+      sum = 0.0f;
+      v = f32x4{0, 0, 0, 0};
+      for (int k = 0; k < turns; ++k) {
+        const f32x2 st = stats[threadIdx.x + (k - turn) * lanes];
+        const float f = __builtin_amdgcn_exp2f(st[0] - all);
+        sum += f * st[1];
+        v += f * sums[threadIdx.x + (k - turn) * lanes];
       }
     }
+    if (!live || turn) continue;
+    const float f = sum != 0.0f ? 1.0f / sum : 0.0f;
+    const f16x2 lo = {(_Float16)(v[0] * f), (_Float16)(v[1] * f)};
+    const f16x2 hi = {(_Float16)(v[2] * f), (_Float16)(v[3] * f)};
+    const long long m = unit.w.start + row / u.group;
+    *reinterpret_cast<u32x2*>(a.out + m * a.out_stride +
+                              (head * u.group + row % u.group) * D + channel) =
+        u32x2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
   }
-  sums[threadIdx.x] = v;
-  stats[threadIdx.x] = f32x2{top, sum};
-  __syncthreads();
-  if (!live || turn) return;
-  float all = kNone;
-  for (int k = 0; k < turns; ++k) all = fmaxf(all, stats[threadIdx.x + k * lanes][0]);
-  sum = 0.0f;
-  v = f32x4{0, 0, 0, 0};
-  for (int k = 0; k < turns; ++k) {
-    const f32x2 st = stats[threadIdx.x + k * lanes];
-    const float f = __builtin_amdgcn_exp2f(st[0] - all);
-    sum += f * st[1];
-    v += f * sums[threadIdx.x + k * lanes];
-  }
-  const float f = sum != 0.0f ? 1.0f / sum : 0.0f;
-  const f16x2 lo = {(_Float16)(v[0] * f), (_Float16)(v[1] * f)};
-  const f16x2 hi = {(_Float16)(v[2] * f), (_Float16)(v[3] * f)};
-  const long long m = unit.w.start + row / u.group;
-  *reinterpret_cast<u32x2*>(a.out + m * a.out_stride +
-                            (head * u.group + row % u.group) * D + channel) =
-      u32x2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
 }
 
 // ---- host ------------------------------------------------------------------------
 
-struct Shape {
+// Sequences of up to kFewRows q rows (rows times heads of a group) run on the
+// kernel above, in blocks of 16 or 32; the others on the kernel for many rows.
+constexpr int kFewRows = 64;
+constexpr int kAny = 0x7FFFFFFF;
+
+// What one of the two kernels does of a batch.
+struct Part {
   UnitShape u;
-  int columns;       // C
   long long blocks;  // of the grid: units that a batch of these sizes may have, times kv heads
   long long slots;   // partial results
   int most_rows;     // of a row block
 };
 
-Shape shape_of(const PagedCache& c, const PagedBatch& b, int heads, int window, int cus) {
-  Shape s;
-  s.u.group = heads / c.kv_heads;
-  s.columns = (long long)b.max_rows * s.u.group > 16 ? 2 : 1;
-  s.u.rows = 16 * s.columns;
-  s.u.window = window > 1 << 30 ? 0 : window;  // no position is further
-  s.most_rows = (int)std::min<long long>(s.u.rows, (long long)b.max_rows * s.u.group);
-  // blocks that a compute unit holds at a time
-  const int resident = s.columns == 1 ? 3 : 2;
-  const char* tm = getenv("TUNE_T");
-  s.u.target = std::max(1, (int)(cus * resident * (tm ? atof(tm) : 1.0)) / c.kv_heads);
+// `resident`: blocks that a compute unit holds at a time.
+Part part_of(const PagedCache& c, const PagedBatch& b, int heads, int window, int cus, int rows,
+             int resident, int low, int high) {
+  Part p;
+  p.u.group = heads / c.kv_heads;
+  p.u.rows = rows;
+  p.u.window = window > 1 << 30 ? 0 : window;  // no position is further
+  p.u.target = std::max(1, cus * resident / c.kv_heads);
+  p.u.low = low;
+  p.u.high = high;
+  p.most_rows = (int)std::min<long long>(rows, (long long)b.max_rows * p.u.group);
   // every sequence's last row block may be ragged
-  const long long row_blocks =
-      (long long)b.M * s.u.group / s.u.rows + std::min(b.B, b.M);
+  const long long row_blocks = (long long)b.M * p.u.group / rows + std::min(b.B, b.M);
   const long long tiles = (((long long)b.max_pages << c.page_shift) + kTile - 1) / kTile;
   const long long ranges = (tiles + kMinTiles - 1) / kMinTiles;
-  s.slots = ranges > 1 ? std::min<long long>(2 * s.u.target, row_blocks * ranges) : 0;
-  s.blocks = std::min(row_blocks + s.u.target, row_blocks * ranges) * c.kv_heads;
+  p.slots = ranges > 1 ? std::min<long long>(2 * p.u.target, row_blocks * ranges) : 0;
+  p.blocks = std::min(row_blocks + p.u.target, row_blocks * ranges) * c.kv_heads;
+  return p;
+}
+
+struct Shape {
+  Part few, many;
+  bool any_few, any_many;
+  int columns;  // C of the kernel for few rows
+};
+
+Shape shape_of(const PagedCache& c, const PagedBatch& b, int heads, int window, int cus) {
+  const long long most = (long long)b.max_rows * (heads / c.kv_heads);
+  Shape s;
+  s.any_many = most > kFewRows;
+  // Sequences of few rows among others get a launch of their own, except where most
+  // sequences must have about as many rows as the longest
+  s.any_few = !s.any_many || 4ll * b.M < 3ll * b.B * b.max_rows;
+  s.columns = most > 16 ? 2 : 1;
+  s.few = part_of(c, b, heads, window, cus, 16 * s.columns, s.columns == 1 ? 3 : 2, 0,
+                  s.any_many ? kFewRows : kAny);
+  s.many = part_of(c, b, heads, window, cus, kManyRows, 2, s.any_few ? kFewRows : 0, kAny);
   return s;
 }
 
+size_t partial_floats(const PagedCache& c, const Part& p) {
+  return (size_t)p.slots * c.kv_heads * p.u.rows * (c.head_dim + 2);
+}
+
+Partials partials_at(float* at, const PagedCache& c, const Part& p) {
+  return {at, at + p.slots * c.kv_heads * p.u.rows * c.head_dim, (uint32_t)p.slots};
+}
+
+// Row blocks with several ranges, times kv heads: half the slots at most, and no
+// more than there are.
+unsigned split_blocks(const PagedCache& c, const Part& p) {
+  return (unsigned)(std::min(p.slots / 2, p.blocks / c.kv_heads) * c.kv_heads);
+}
+
 template <int D, int G>
-void launch_columns(const PagedCache& c, const PagedBatch& b, const AttentionArgs& a,
-                    const Shape& s, const Partials& part, hipStream_t stream) {
-  const dim3 grid((unsigned)s.blocks), block(64 * kWaves);
+void launch_few(const PagedCache& c, const PagedBatch& b, const AttentionArgs& a, const Shape& s,
+                const Partials& part, hipStream_t stream) {
+  const dim3 grid((unsigned)s.few.blocks), block(64 * kWaves);
   if (s.columns == 1)
-    hipLaunchKernelGGL((kv4_attention_kernel<D, G, 1>), grid, block, 0, stream, c, b, a, s.u, part);
+    hipLaunchKernelGGL((kv4_attention_few_kernel<D, G, 1>), grid, block, 0, stream, c, b, a,
+                       s.few.u, part);
   else
-    hipLaunchKernelGGL((kv4_attention_kernel<D, G, 2>), grid, block, 0, stream, c, b, a, s.u, part);
+    hipLaunchKernelGGL((kv4_attention_few_kernel<D, G, 2>), grid, block, 0, stream, c, b, a,
+                       s.few.u, part);
 }
 
 }  // namespace
@@ -833,37 +704,50 @@ void launch_columns(const PagedCache& c, const PagedBatch& b, const AttentionArg
 const char* attention_refusal(const PagedCache& c, const PagedBatch& b, int heads, int cus) {
   // a launch's threads are counted in 32 bits
   const Shape s = shape_of(c, b, heads, 0, cus);
-  const bool many = (long long)b.M * heads > 1 << 30 || s.blocks >= (1ll << 32) / (64 * kWaves);
+  const bool many = (long long)b.M * heads > 1 << 30 ||
+                    std::max(s.few.blocks, s.many.blocks) >= (1ll << 32) / (64 * kWaves);
   return many ? "too many rows, heads and sequences for a launch" : nullptr;
 }
 
 size_t attention_workspace(const PagedCache& c, const PagedBatch& b, int heads, int cus) {
   const Shape s = shape_of(c, b, heads, 0, cus);
-  return (size_t)s.slots * c.kv_heads * s.u.rows * (c.head_dim + 2) * sizeof(float);
+  return sizeof(float) * ((s.any_few ? partial_floats(c, s.few) : 0) +
+                          (s.any_many ? partial_floats(c, s.many) : 0));
 }
 
 hipError_t launch_kv4_attention(const PagedCache& c, const PagedBatch& b, const AttentionArgs& a,
                                 hipStream_t stream) {
   const Shape s = shape_of(c, b, a.heads, a.window, a.cus);
   float* ws = static_cast<float*>(a.workspace);
-  const Partials part{ws, ws + s.slots * c.kv_heads * s.u.rows * c.head_dim, (uint32_t)s.slots};
-  if (c.head_dim == 128 && c.G == 128)
-    launch_columns<128, 128>(c, b, a, s, part, stream);
-  else if (c.head_dim == 128 && c.G == 64)
-    launch_columns<128, 64>(c, b, a, s, part, stream);
-  else if (c.head_dim == 128)
-    launch_columns<128, 32>(c, b, a, s, part, stream);
-  else if (c.G == 64)
-    launch_columns<64, 64>(c, b, a, s, part, stream);
-  else
-    launch_columns<64, 32>(c, b, a, s, part, stream);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !s.slots) return e;
-  // row blocks with several ranges: half the slots at most, and no more than there are
-  const long long split = std::min<long long>(s.slots / 2, s.blocks / c.kv_heads);
-  hipLaunchKernelGGL(kv4_attention_combine_kernel,
-                     dim3((unsigned)(split * c.kv_heads), std::min(s.u.rows, s.most_rows + 1) / 2),
-                     dim3(256), 0, stream, c, b, a, s.u, part);
+  const Partials few = partials_at(ws, c, s.few);
+  const Partials many = partials_at(ws + (s.any_few ? partial_floats(c, s.few) : 0), c, s.many);
+  hipError_t e = hipSuccess;
+  if (s.any_many) {
+    e = launch_attention_many(c, b, a, s.many.u, many, (unsigned)s.many.blocks, stream);
+    if (e != hipSuccess) return e;
+  }
+  if (s.any_few) {
+    if (c.head_dim == 128 && c.G == 128)
+      launch_few<128, 128>(c, b, a, s, few, stream);
+    else if (c.head_dim == 128 && c.G == 64)
+      launch_few<128, 64>(c, b, a, s, few, stream);
+    else if (c.head_dim == 128)
+      launch_few<128, 32>(c, b, a, s, few, stream);
+    else if (c.G == 64)
+      launch_few<64, 64>(c, b, a, s, few, stream);
+    else
+      launch_few<64, 32>(c, b, a, s, few, stream);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  const unsigned few_blocks = s.any_few ? split_blocks(c, s.few) : 0;
+  const unsigned many_blocks = s.any_many ? split_blocks(c, s.many) : 0;
+  if (few_blocks + many_blocks == 0) return e;
+  auto parts = [](const Part& p, int rows) { return (p.most_rows + rows - 1) / rows; };
+  const int y = std::max(few_blocks ? parts(s.few, kCombineRows) : 0,
+                         many_blocks ? parts(s.many, kCombineManyRows) : 0);
+  hipLaunchKernelGGL(kv4_attention_combine_kernel, dim3(few_blocks + many_blocks, y), dim3(256), 0,
+                     stream, c, b, a, s.few.u, few, s.many.u, many, (int)few_blocks);
   return hipGetLastError();
 }
 

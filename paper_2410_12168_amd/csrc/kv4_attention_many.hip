@@ -1,0 +1,480 @@
+// kv4_attention_many.hip -- causal attention over the paged 4-bit cache for
+// sequences of many new rows (chunks of prompts), gfx950.
+//
+// The mathematics is kv4_attention.hip's.  With many rows the same tokens serve
+// all of them, so a block of four waves shares a tile of 64 tokens: each code
+// becomes an fp16 number in LDS once, and each wave multiplies 32 rows of q with
+// the tile (v_mfma_f32_32x32x16_f16; rows: tokens or channels, columns: rows of
+// q).  A second tile is staged while one is used.
+//
+//   - a code c is the fp16 subnormal c * 2^-24, 16 times that for odd channels;
+//     q takes the 16 back for K, the output for V.  Eight channels of a dword lie
+//     in the order (0, 4, 1, 5, 2, 6, 3, 7) in both tiles.
+//   - token 32 t + 8 a + 4 h + r of a tile is row 8 a + 4 h + r of the t-th score
+//     product, element 4 a + r of half h of the lanes; V's operand for tokens
+//     32 t + 16 u .. + 15 holds 16 u + 8 e + 4 h + r in half h, so again the weights
+//     go from one product into the other in place.  V's rows hold channels, its
+//     operand tokens: the transposing read (ds_read_b64_tr_b16: 4 rows of 16 fp16)
+//     turns them.
+//   - 16-byte chunks of a row in LDS change places with the row's number, so that
+//     the reads and writes of 16 lanes meet all banks.
+#include "attention.h"
+
+namespace comet {
+
+namespace {
+
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+// Maximum and sum over the two lanes of a column (l, l ^ 32).
+__device__ inline float pair_max(float v) {
+  uint32_t a = __float_as_uint(v), b = a;
+  swap32(a, b);
+  return fmaxf(__uint_as_float(a), __uint_as_float(b));
+}
+__device__ inline float pair_sum(float v) {
+  uint32_t a = __float_as_uint(v), b = a;
+  swap32(a, b);
+  return __uint_as_float(a) + __uint_as_float(b);
+}
+
+template <int D, int G>
+__global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
+    PagedCache c, PagedBatch b, AttentionArgs a, UnitShape u, Partials part) {
+  constexpr int NG = D / G;
+  constexpr int KS = D / 16;  // steps of the score product
+  constexpr int DT = D / 32;  // 32-channel tiles of the output
+  constexpr int ROW = D / 2;  // bytes of a row of codes
+  constexpr int KD = D / 32;  // dwords of codes that a thread turns into fp16
+  constexpr int F = 2 * D;    // bytes of a row of fp16
+  constexpr int PARAMS = 4 * NG * kTile;  // [NG][K's s, mn, V's s, mn][64]
+  // of each of the two buffers: K, V, parameters
+  constexpr int V_AT = kTile * F, P_AT = 2 * kTile * F, BUF = P_AT + 4 * PARAMS;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[2 * BUF];
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 31, half = lane >> 5;
+  const int head = blockIdx.x % c.kv_heads;
+  Unit unit;
+  if (!find_unit<false>(b, c.page_shift, u, blockIdx.x / c.kv_heads, &unit)) return;
+  const SeqWork& w = unit.w;
+  const int row0 = unit.block * u.rows;  // of n * group
+  const int rows = min(u.rows, w.n * u.group - row0);
+  // positions of the block's first and last rows
+  const int pos0 = w.len - w.n + row0 / u.group;
+  const int pos1 = w.len - w.n + (row0 + rows - 1) / u.group;
+  const int cap = b.max_pages << c.page_shift;
+  // the unit's share of the sequence's tiles, without those its rows do not see
+  const uint32_t each = w.tiles / unit.ranges, more = w.tiles % unit.ranges;
+  int tile0 = w.first + unit.range * each + min(unit.range, more);
+  int tile1 = tile0 + each + (unit.range < more);
+  if (pos1 < 0)
+    tile1 = 0;
+  else
+    tile1 = min(tile1, min(pos1, cap - 1) / kTile + 1);
+  if (u.window > 0) tile0 = max(tile0, max(0, pos0 - u.window + 1) / kTile);
+
+  // ---- this wave's rows
+  const int wave_row = 32 * wave;
+  const int wave_rows = min(32, rows - wave_row);  // 0 or less: none
+  const int wave_pos0 = w.len - w.n + (row0 + wave_row) / u.group;
+  const int wave_pos1 = w.len - w.n + (row0 + wave_row + max(wave_rows, 1) - 1) / u.group;
+  const bool live = col < wave_rows;
+  const int seq_row = (row0 + wave_row + col) / u.group;
+  const int q_head = head * u.group + (row0 + wave_row + col) % u.group;
+  const int pos = w.len - w.n + seq_row;
+  f16x8 q[KS];
+  float qsum[NG], offset[NG];
+  float big = 0.0f;
+  u32x4 raw[KS];
+  #pragma unroll
+  for (int s = 0; s < KS; ++s) {
+    raw[s] = u32x4{0, 0, 0, 0};
+    if (live)
+      raw[s] = *reinterpret_cast<const u32x4*>(a.Q + (long long)(w.start + seq_row) * a.q_stride +
+                                               q_head * D + 16 * s + 8 * half);
+    #pragma unroll
+    for (int k = 0; k < 4; ++k)
+      big = fmaxf(big, fmaxf(fabsf(low_half(raw[s][k])), fabsf(low_half(raw[s][k] >> 16))));
+  }
+  big = pair_max(big);
+  int e = 10;
+  if (big > 0.0f && big < INFINITY) e = ilogbf(big);
+  const float qf = ldexpf(a.scale < 0.0f ? -1.0f : 1.0f, 10 - e);
+  // above 0, so that an unseen token's -infinity stays one
+  const float kappa = fmaxf(ldexpf(fabsf(a.scale) * kLog2e, 24 + e - 10), 0x1p-120f);
+  #pragma unroll
+  for (int g = 0; g < NG; ++g) qsum[g] = offset[g] = 0.0f;
+  #pragma unroll
+  for (int s = 0; s < KS; ++s) {
+    float v[8];
+    float sum = 0.0f;
+    #pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      v[2 * k] = low_half(raw[s][k]) * qf;
+      v[2 * k + 1] = low_half(raw[s][k] >> 16) * qf;
+      sum += v[2 * k] + v[2 * k + 1];
+    }
+    qsum[16 * s / G] += sum;
+    q[s] = f16x8{(_Float16)v[0],            (_Float16)v[4],
+                 (_Float16)(v[1] * 0.0625f), (_Float16)(v[5] * 0.0625f),
+                 (_Float16)v[2],            (_Float16)v[6],
+                 (_Float16)(v[3] * 0.0625f), (_Float16)(v[7] * 0.0625f)};
+  }
+  #pragma unroll
+  for (int g = 0; g < NG; ++g) qsum[g] = pair_sum(qsum[g]) * 0x1p-24f;
+  float top = kNone, weight_sum = 0.0f;
+  f32x16 o[DT];
+  #pragma unroll
+  for (int d = 0; d < DT; ++d)
+    #pragma unroll
+    for (int k = 0; k < 16; ++k) o[d][k] = 0.0f;
+  int vexp = -24;  // exponent of the largest scale of V so far, the same in all waves
+
+  // ---- pages: lane 4 i + k has the one of granule k (16 tokens) of the i-th next
+  // tile, or -1
+  const int32_t* table = b.block_table + (long long)unit.seq * b.max_pages;
+  int pages = -1;
+  auto load_pages = [&](int tile) {
+    const int i = (tile * kTile + 16 * lane) >> c.page_shift;
+    const int page = i < b.max_pages ? table[i] : -1;
+    pages = (unsigned)page < (unsigned)c.num_pages ? page : -1;
+  };
+  // ---- loads of a tile: a thread takes a quarter of the codes of one token of its
+  // wave's granule, and the parameters of token `lane`
+  const int token = 16 * wave + (lane & 15), quarter = lane >> 4;
+  uint32_t kreg[KD], vreg[KD], preg[2][NG];
+  unsigned long long held = 0;  // tokens that are in the cache
+  auto load = [&](int tile, int ahead) {
+    auto row_of = [&](int k) {
+      const int page = __builtin_amdgcn_readlane(pages, 4 * ahead + k);
+      return cache_row(c, max(page, 0), head, tile * kTile + 16 * k);
+    };
+    const long long row = row_of(wave);
+    const unsigned at = (lane & 15) * ROW + ROW / 4 * quarter;
+    if constexpr (KD == 4) {
+      const u32x4 k = *reinterpret_cast<const u32x4*>(c.k_codes + row * ROW + at);
+      const u32x4 v = *reinterpret_cast<const u32x4*>(c.v_codes + row * ROW + at);
+      #pragma unroll
+      for (int i = 0; i < 4; ++i) kreg[i] = k[i], vreg[i] = v[i];
+    } else {
+      const u32x2 k = *reinterpret_cast<const u32x2*>(c.k_codes + row * ROW + at);
+      const u32x2 v = *reinterpret_cast<const u32x2*>(c.v_codes + row * ROW + at);
+      #pragma unroll
+      for (int i = 0; i < 2; ++i) kreg[i] = k[i], vreg[i] = v[i];
+    }
+    const long long r0 = row_of(0), r1 = row_of(1), r2 = row_of(2), r3 = row_of(3);
+    const long long mine = quarter < 2 ? (quarter == 0 ? r0 : r1) : (quarter == 2 ? r2 : r3);
+    const long long p = (mine + (lane & 15)) * NG;
+    #pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      preg[0][g] = reinterpret_cast<const uint32_t*>(c.k_params)[p + g];
+      preg[1][g] = reinterpret_cast<const uint32_t*>(c.v_params)[p + g];
+    }
+    held = 0;
+    #pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (__builtin_amdgcn_readlane(pages, 4 * ahead + k) >= 0) held |= 0xFFFFull << (16 * k);
+    const int left = w.len - tile * kTile;
+    if (left < kTile) held &= (1ull << max(left, 0)) - 1;
+  };
+
+  // Where a 16-byte chunk (8 channels) of a token lies in LDS.
+  auto k_place = [](int t, int chunk) {
+    return t * F + 16 * (chunk ^ (D == 128 ? t & 15 : t >> 1 & 7));
+  };
+  auto v_place = [](int t, int chunk) {
+    const int turn = D == 128 ? 4 * (t & 3) + (t >> 2 & 3) : 4 * (t >> 1 & 1) + (t >> 2 & 3);
+    return t * F + 16 * (chunk ^ turn);
+  };
+
+  // ---- the loaded tile into LDS; returns the exponent of the scale of the weights
+  unsigned long long poison_next = 0;
+  auto stage = [&](int buf, int exponent) {
+    #pragma unroll
+    for (int i = 0; i < KD; ++i) {
+      *reinterpret_cast<f16x8*>(lds + buf + k_place(token, KD * quarter + i)) =
+          codes_f16(kreg[i]);
+      *reinterpret_cast<f16x8*>(lds + buf + V_AT + v_place(token, KD * quarter + i)) =
+          codes_f16(vreg[i]);
+    }
+    const bool stored = held >> lane & 1;
+    bool bad = false;
+    #pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      preg[0][g] = stored ? preg[0][g] : 0u;
+      preg[1][g] = stored ? preg[1][g] : 0u;
+      bad |= not_finite(preg[0][g]) || not_finite(preg[1][g]);
+    }
+    // tokens that are not finite make the rows that see them not-a-number, and no
+    // others: they count as zeros in the products
+    poison_next = __ballot(bad);
+    uint32_t bits = 0;
+    #pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      preg[0][g] = bad ? 0u : preg[0][g];
+      preg[1][g] = bad ? 0u : preg[1][g];
+      bits = max(bits, preg[1][g] & 0xFFFFu);
+    }
+    const float vbig = low_half(bits);
+    if (__any(vbig >= ldexpf(1.0f, exponent + 1))) {
+      float m = vbig;
+      #pragma unroll
+      for (int s = 1; s < 64; s <<= 1) m = fmaxf(m, __shfl_xor(m, s));
+      exponent = __builtin_amdgcn_readfirstlane(ilogbf(m));
+    }
+    // the waves take turns at the parameters, which all of them have
+    const float unit_w = ldexpf(1.0f, 14 - exponent);
+    #pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      float* at = reinterpret_cast<float*>(lds + buf + P_AT) + 4 * g * kTile + lane;
+      if (wave == (2 * g & 3)) {
+        at[0] = low_half(preg[0][g]);
+        at[kTile] = low_half(preg[0][g] >> 16);
+      }
+      if (wave == (2 * g + 1 & 3)) {
+        at[2 * kTile] = low_half(preg[1][g]) * unit_w;
+        at[3 * kTile] = low_half(preg[1][g] >> 16);
+      }
+    }
+    return exponent;
+  };
+
+  // ---- 32 rows of q times a tile
+  const int lane16 = lane & 15;
+  // this lane's chunk 0 of K's row `col`, and of V's row for the transposing reads;
+  // other chunks differ by exclusive or
+  const int k_at = k_place(col, half);
+  const int v_at = V_AT + v_place(4 * half + (lane16 >> 2),
+                                  2 * (lane >> 4 & 1) + (lane16 >> 1 & 1)) + 8 * (lane16 & 1);
+  auto work = [&](int buf, int tile, unsigned long long have, unsigned long long poison) {
+    const int t0 = tile * kTile;
+    const float* params = reinterpret_cast<const float*>(lds + buf + P_AT);
+    if (poison && seen_tokens(pos, t0, u.window, poison)) weight_sum = NAN;
+    f32x16 x[2];
+    f16x8 k[KS];
+    const uint8_t* k_row = lds + buf;
+    #pragma unroll
+    for (int s = 0; s < KS; ++s)
+      k[s] = *reinterpret_cast<const f16x8*>(k_row + (k_at ^ 32 * s));
+    #pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      __builtin_amdgcn_sched_barrier(0);  // the reads above all come first
+      #pragma unroll
+      for (int g = 0; g < NG; ++g) {
+        f32x16 dot;
+        #pragma unroll
+        for (int i = 0; i < 16; ++i) dot[i] = 0.0f;
+        #pragma unroll
+        for (int s = g * KS / NG; s < (g + 1) * KS / NG; ++s) {
+          dot = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[s], q[s], dot, 0, 0, 0);
+          if (t == 0)
+            k[s] = *reinterpret_cast<const f16x8*>(k_row + (k_at ^ 32 * s) + 32 * F);
+        }
+        #pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float* at = params + 4 * g * kTile + 32 * t + 8 * i + 4 * half;
+          const f32x4 s = *reinterpret_cast<const f32x4*>(at);
+          const f32x4 mn = *reinterpret_cast<const f32x4*>(at + kTile);
+          #pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const float rest = g ? fmaf(mn[r], qsum[g], x[t][4 * i + r]) : mn[r] * qsum[g];
+            x[t][4 * i + r] = fmaf(s[r], dot[4 * i + r], rest);
+          }
+        }
+      }
+    }
+    #pragma unroll
+    for (int t = 0; t < 2; ++t) asm volatile("" : "+v"(x[t]));  // see kv4_attention.hip
+    // V's operand for 16 tokens of a 32-channel tile
+    const uint8_t* v_row = lds + buf;
+    auto v_operand = [&](int st, int d) {
+      i16x4 v[2];
+      #pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        v[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (__attribute__((address_space(3))) i16x4*)(v_row + (v_at ^ 64 * d + 32 * i) +
+                                                       (16 * st + 8 * i) * F));
+      }
+      return __builtin_bit_cast(f16x8,
+                                __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    f16x8 v[DT];
+    #pragma unroll
+    for (int d = 0; d < DT; ++d) v[d] = v_operand(0, d);
+    __builtin_amdgcn_sched_barrier(0);
+    const bool whole = have == ~0ull && t0 + kTile - 1 <= wave_pos0 &&
+                       (u.window == 0 || t0 > wave_pos1 - u.window);
+    if (!whole) {
+      const unsigned long long seen = seen_tokens(pos, t0, u.window, have) >> (4 * half);
+      #pragma unroll
+      for (int t = 0; t < 2; ++t)
+        #pragma unroll
+        for (int k = 0; k < 16; ++k)
+          if (!((uint32_t)(seen >> 32 * t) >> (8 * (k / 4) + k % 4) & 1u)) x[t][k] = -INFINITY;
+    }
+    // running maximum; what was added up before shrinks with it
+    float m = x[0][0];
+    #pragma unroll
+    for (int k = 1; k < 32; ++k) m = fmaxf(m, x[k / 16][k % 16]);
+    const float next = fmaxf(top, pair_max(m) * kappa);
+    if (__any(next > top)) {
+      const float f = __builtin_amdgcn_exp2f(top - next);
+      top = next;
+      weight_sum *= f;
+      #pragma unroll
+      for (int g = 0; g < NG; ++g) offset[g] *= f;
+      #pragma unroll
+      for (int d = 0; d < DT; ++d) o[d] *= f;
+    }
+    #pragma unroll
+    for (int t = 0; t < 2; ++t)
+      #pragma unroll
+      for (int k = 0; k < 16; ++k) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(x[t][k], kappa, -top));
+        x[t][k] = p;
+        weight_sum += p;
+      }
+    // the weighted sum, 16 tokens at a time
+    #pragma unroll
+    for (int st = 0; st < 4; ++st) {
+      #pragma unroll
+      for (int g = 0; g < NG; ++g) {
+        f16x8 p;
+        #pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const float* at = params + (4 * g + 2) * kTile + 16 * st + 8 * i + 4 * half;
+          const f32x4 s = *reinterpret_cast<const f32x4*>(at);
+          const f32x4 mn = *reinterpret_cast<const f32x4*>(at + kTile);
+          #pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const float wt = x[st / 2][8 * (st & 1) + 4 * i + r];
+            offset[g] = fmaf(wt, mn[r], offset[g]);
+            p[4 * i + r] = (_Float16)(wt * s[r]);
+          }
+        }
+        #pragma unroll
+        for (int d = g * DT / NG; d < (g + 1) * DT / NG; ++d) {
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[d], p, o[d], 0, 0, 0);
+          if (st < 3) v[d] = v_operand(st + 1, d);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+
+  if (tile0 < tile1) {
+    load_pages(tile0);
+    load(tile0, 0);
+    int exponent = stage(0, vexp);
+    unsigned long long have = held, poison = poison_next;
+    if (tile0 + 1 < tile1) load(tile0 + 1, 1);
+    int ahead = 1;  // where in `pages` the loaded tile is
+    for (int tile = tile0; tile < tile1; ++tile) {
+      const int buf = (tile - tile0) & 1 ? BUF : 0;
+      __syncthreads();  // the tile is in LDS, and the other buffer is free
+      int exponent_next = exponent;
+      unsigned long long have_next = 0;
+      if (tile + 1 < tile1) {
+        exponent_next = stage(BUF - buf, exponent);
+        have_next = held;
+        if (tile + 2 < tile1) {
+          if (++ahead == 16) {
+            load_pages(tile + 2);
+            ahead = 0;
+          }
+          load(tile + 2, ahead);
+        }
+      }
+      const int t0 = tile * kTile;
+      const bool some = wave_rows > 0 && t0 <= wave_pos1 &&
+                        (u.window == 0 || t0 + kTile - 1 > wave_pos0 - u.window);
+      if (some) {
+        if (exponent != vexp) {
+          const float f = ldexpf(1.0f, vexp - exponent);
+          vexp = exponent;
+          #pragma unroll
+          for (int d = 0; d < DT; ++d) o[d] *= f;
+        }
+        work(buf, tile, have, poison);
+      }
+      exponent = exponent_next;
+      have = have_next;
+      poison = poison_next;
+    }
+  }
+
+  // ---- out: element 4 i + r of half h is channel (0, 4, 1, 5)[r] + 2 h of chunk
+  // 4 d + i; two chunks change halves, so that a lane has the 8 channels of one
+  const float sum = pair_sum(weight_sum);
+  const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
+  const float factor = ldexpf(1.0f, 24 - 14 + vexp);
+  #pragma unroll
+  for (int g = 0; g < NG; ++g) offset[g] = pair_sum(offset[g]);
+  const bool partial = unit.ranges > 1;
+  if (partial && unit.slot >= part.slots) return;  // no batch that comet.h allows
+  const long long at =
+      ((long long)unit.slot * c.kv_heads + head) * u.rows + wave_row + col;
+  if (partial && live && half == 0)
+    *reinterpret_cast<f32x2*>(part.stats + at * 2) = f32x2{top, sum};
+  uint16_t* out = a.out + (long long)(w.start + seq_row) * a.out_stride + q_head * D;
+  #pragma unroll
+  for (int d = 0; d < DT; ++d)
+    #pragma unroll
+    for (int i = 0; i < 4; i += 2) {
+      float lo[4], hi[4];
+      #pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float f = r < 2 ? factor : factor * 0.0625f;
+        uint32_t va = __float_as_uint(fmaf(o[d][4 * i + r], f, offset[32 * d / G]));
+        uint32_t vb = __float_as_uint(fmaf(o[d][4 * i + 4 + r], f, offset[32 * d / G]));
+        swap32(va, vb);
+        lo[r] = __uint_as_float(va);
+        hi[r] = __uint_as_float(vb);
+      }
+      if (live) {
+        const int channel = 8 * (4 * d + i + half);
+        const f32x4 y0 = {lo[0], lo[2], hi[0], hi[2]}, y1 = {lo[1], lo[3], hi[1], hi[3]};
+        if (partial) {
+          *reinterpret_cast<f32x4*>(part.sums + at * D + channel) = y0;
+          *reinterpret_cast<f32x4*>(part.sums + at * D + channel + 4) = y1;
+        } else {
+          f16x8 y;
+          #pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            y[k] = (_Float16)(y0[k] * inv);
+            y[4 + k] = (_Float16)(y1[k] * inv);
+          }
+          *reinterpret_cast<f16x8*>(out + channel) = y;
+        }
+      }
+    }
+}
+
+template <int D, int G>
+void launch(const PagedCache& c, const PagedBatch& b, const AttentionArgs& a, const UnitShape& u,
+            const Partials& part, unsigned blocks, hipStream_t stream) {
+  hipLaunchKernelGGL((kv4_attention_many_kernel<D, G>), dim3(blocks), dim3(64 * kWaves), 0, stream,
+                     c, b, a, u, part);
+}
+
+}  // namespace
+
+hipError_t launch_attention_many(const PagedCache& c, const PagedBatch& b, const AttentionArgs& a,
+                                 const UnitShape& u, const Partials& part, unsigned blocks,
+                                 hipStream_t stream) {
+  if (c.head_dim == 128 && c.G == 128)
+    launch<128, 128>(c, b, a, u, part, blocks, stream);
+  else if (c.head_dim == 128 && c.G == 64)
+    launch<128, 64>(c, b, a, u, part, blocks, stream);
+  else if (c.head_dim == 128)
+    launch<128, 32>(c, b, a, u, part, blocks, stream);
+  else if (c.G == 64)
+    launch<64, 64>(c, b, a, u, part, blocks, stream);
+  else
+    launch<64, 32>(c, b, a, u, part, blocks, stream);
+  return hipGetLastError();
+}
+
+}  // namespace comet
