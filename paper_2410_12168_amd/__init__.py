@@ -352,7 +352,7 @@ def _struct(s):
     """A KV4Cache or KV4Batch as the address of its struct (None stays null)."""
     if s is None:
         return None
-    return ctypes.addressof(s.struct if hasattr(s, "struct") else s)
+    return s.address if hasattr(s, "address") else ctypes.addressof(s)
 
 
 def _kv4_row_room(cache, batch, K, V, k_stride: int, v_stride: int) -> None:
@@ -604,34 +604,77 @@ def rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "none",
     return freqs, float(mscale[0])
 
 
-def _heads_of(t, name: str):
-    """(rows, heads, channels, row stride) of a float16 tensor [rows][heads][channels]
-    on the current device whose heads are contiguous; the rows may lie in a wider
-    buffer (the q, k or v columns of a qkv output)."""
+# torch and its lookup of the current device, once a wrapper below has needed
+# them.  These wrappers run several times per layer and token, so an argument that
+# is as it should be passes with few lookups.  (rope of one token: 6.5 us a call
+# when each check was made by itself, of which the library's own part is 3.3.)
+_torch = None
+_current_device = None
+_float16 = None
+
+
+def _need_torch():
+    global _torch, _current_device, _float16
     import torch
 
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != torch.float16 or t.dim() != 3:
-        got = (f"{t.dtype} {tuple(t.shape)} on {t.device}" if isinstance(t, torch.Tensor)
+    _float16 = torch.float16
+    if not torch.cuda.is_available():
+        _current_device = lambda: -2  # where no tensor is
+    else:
+        torch.cuda.current_device()  # initializes the device
+        _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+    _torch = torch
+    return _current_device()
+
+
+def _forget_torch():
+    global _torch
+    _torch = None
+
+
+os.register_at_fork(after_in_child=_forget_torch)
+
+
+def _here() -> int:
+    """The current device's number, which a call's tensors must be on."""
+    return _need_torch() if _torch is None else _current_device()
+
+
+def _heads_of(t, name: str, here: int):
+    """(rows, heads, channels, row stride) of a float16 tensor [rows][heads][channels]
+    on device `here` whose heads are contiguous; the rows may lie in a wider buffer
+    (the q, k or v columns of a qkv output)."""
+    try:
+        M, H, D = t.shape
+        s0, s1, s2 = t.stride()
+        fits = t.dtype is _float16 and t.get_device() == here
+    except (AttributeError, TypeError, ValueError):
+        fits = False
+    if not fits:
+        _explain(t, name, here)
+        got = (f"{t.dtype} {tuple(t.shape)} on {t.device}" if isinstance(t, _torch.Tensor)
                else type(t).__name__)
         raise ValueError(f"{name}: need a float16 CUDA tensor [rows][heads][channels], got {got}")
-    M, H, D = t.shape
-    s0, s1, s2 = t.stride()
-    if (D > 1 and s2 != 1) or (H > 1 and s1 != D) or (M > 1 and s0 < H * D):
+    if s2 == 1 and s1 == D and s0 >= H * D:
+        return M, H, D, s0
+    if (s2 != 1 and D > 1) or (s1 != D and H > 1) or (s0 < H * D and M > 1):
         raise ValueError(f"{name}: heads and channels must be contiguous and rows apart, got "
                          f"strides {t.stride()} for {tuple(t.shape)}")
-    if M == 1:
-        s0 = H * D  # of no meaning then
-    return M, H, D, s0
+    return M, H, D, max(s0, H * D) if M > 1 else H * D
 
 
-def _on_current(*named) -> None:
-    """The tensors are on the device that the call will run on."""
-    import torch
+def _explain(t, name: str, here: int) -> None:
+    """Raises for a tensor on another GPU."""
+    at = t.get_device() if hasattr(t, "get_device") else -1
+    if at >= 0 and at != here:
+        raise ValueError(f"{name}: on device {at}, the current device is {here}")
 
-    at = torch.cuda.current_device()
-    for name, index in named:
-        if index != at:
-            raise ValueError(f"{name}: on device {index}, the current device is {at}")
+
+def _plain(t, dtype: str, name: str, here: int) -> None:
+    """_tensor, on device `here`."""
+    _tensor(t, dtype, name)
+    if t.get_device() != here:
+        _explain(t, name, here)
 
 
 def _new(shape, dtype, device, stream):
@@ -651,21 +694,20 @@ def rope(x, positions, freqs, interleaved: bool = False, mscale: float = 1.0, ou
     """Rotary positions.  x: float16 CUDA tensor [M][heads][head_dim] (rows may lie in a
     wider buffer); positions: int32 [M]; freqs: float64 [rot_dim / 2], of
     ``rope_frequencies``, on the GPU.  Returns out (out=x rotates in place)."""
-    import torch
-
-    M, H, D, xs = _heads_of(x, "x")
-    _tensor(positions, "int32", "positions")
-    _tensor(freqs, "float64", "freqs")
+    here = _here()
+    M, H, D, xs = _heads_of(x, "x", here)
+    _plain(positions, "int32", "positions", here)
+    _plain(freqs, "float64", "freqs", here)
     _exact(positions, M, "positions")
     if out is None:
-        out = _new((M, H, D), torch.float16, x.device, stream)
-    oM, oH, oD, os_ = _heads_of(out, "out")
-    if (oM, oH, oD) != (M, H, D):
-        raise ValueError(f"out: shape {tuple(out.shape)}, expected {(M, H, D)}")
-    _on_current(("x", x.get_device()), ("positions", positions.get_device()),
-                ("freqs", freqs.get_device()), ("out", out.get_device()))
+        out = _new((M, H, D), _torch.float16, x.device, stream)
+        os_ = H * D
+    else:
+        oM, oH, oD, os_ = _heads_of(out, "out", here)
+        if oM != M or oH != H or oD != D:
+            raise ValueError(f"out: shape {tuple(out.shape)}, expected {(M, H, D)}")
     _check(lib().comet_rope(x.data_ptr(), positions.data_ptr(), freqs.data_ptr(), out.data_ptr(),
-                            M, H, D, 2 * freqs.numel(), xs, os_, int(bool(interleaved)), mscale,
+                            M, H, D, 2 * freqs.numel(), xs, os_, 1 if interleaved else 0, mscale,
                             _stream(stream)))
     return out
 
@@ -702,6 +744,7 @@ class KV4Cache:
         self.struct = KV4CacheStruct(k_codes.data_ptr(), k_params.data_ptr(), v_codes.data_ptr(),
                                      v_params.data_ptr(), pages, size, heads, self.head_dim,
                                      self.G)
+        self.address = ctypes.addressof(self.struct)
 
     @classmethod
     def empty(cls, num_pages: int, page_size: int, kv_heads: int, head_dim: int, G: int = 128,
@@ -741,12 +784,22 @@ class KV4Batch:
         self.device = seq_lens.device
         self.struct = KV4BatchStruct(row_start.data_ptr(), seq_lens.data_ptr(),
                                      block_table.data_ptr(), B, M, self.max_pages, self.max_rows)
+        self.address = ctypes.addressof(self.struct)
 
 
-def _kv4_rows(t, cache, batch, name: str):
+def _kv4_here(cache, batch) -> int:
+    """The current device's number, which the cache and the batch must be on."""
+    here = _here()
+    if cache.device.index != here or batch.device.index != here:
+        raise ValueError(f"cache on {cache.device}, batch on {batch.device}, the current device "
+                         f"is {here}")
+    return here
+
+
+def _kv4_rows(t, cache, batch, name: str, here: int):
     """Row stride of a K or V buffer of this cache and batch."""
-    M, H, D, stride = _heads_of(t, name)
-    if (M, H, D) != (batch.M, cache.kv_heads, cache.head_dim):
+    M, H, D, stride = _heads_of(t, name, here)
+    if M != batch.M or H != cache.kv_heads or D != cache.head_dim:
         raise ValueError(f"{name}: shape {tuple(t.shape)}, expected "
                          f"{(batch.M, cache.kv_heads, cache.head_dim)}")
     return stride
@@ -755,27 +808,26 @@ def _kv4_rows(t, cache, batch, name: str):
 def kv4_append(cache: KV4Cache, batch: KV4Batch, k, v, stream=None) -> None:
     """Quantizes the rows k, v (float16 [M][kv_heads][head_dim], rows may lie in a wider
     buffer) into the cache, each to its sequence's last positions."""
-    ks, vs = _kv4_rows(k, cache, batch, "k"), _kv4_rows(v, cache, batch, "v")
-    _on_current(("cache", cache.device.index), ("batch", batch.device.index),
-                ("k", k.get_device()), ("v", v.get_device()))
-    _check(lib().comet_kv4_append(ctypes.addressof(cache.struct), ctypes.addressof(batch.struct),
-                                  k.data_ptr(), v.data_ptr(), ks, vs, _stream(stream)))
+    here = _kv4_here(cache, batch)
+    ks, vs = _kv4_rows(k, cache, batch, "k", here), _kv4_rows(v, cache, batch, "v", here)
+    _check(lib().comet_kv4_append(cache.address, batch.address, k.data_ptr(), v.data_ptr(), ks, vs,
+                                  _stream(stream)))
 
 
 def kv4_gather(cache: KV4Cache, batch: KV4Batch, k_out=None, v_out=None, stream=None):
     """Reads the last rows of each sequence back: (k, v) float16 [M][kv_heads][head_dim].
     Rows in no sequence are left as they are (uninitialized in a new tensor)."""
-    import torch
-
+    here = _kv4_here(cache, batch)
     shape = (batch.M, cache.kv_heads, cache.head_dim)
-    k, v = (_new(shape, torch.float16, cache.device, stream) if t is None else t
-            for t in (k_out, v_out))
-    ks, vs = _kv4_rows(k, cache, batch, "k_out"), _kv4_rows(v, cache, batch, "v_out")
-    _on_current(("cache", cache.device.index), ("batch", batch.device.index),
-                ("k_out", k.get_device()), ("v_out", v.get_device()))
-    _check(lib().comet_kv4_gather(ctypes.addressof(cache.struct), ctypes.addressof(batch.struct),
-                                  k.data_ptr(), v.data_ptr(), ks, vs, _stream(stream)))
-    return k, v
+    if k_out is None:
+        k_out = _new(shape, _torch.float16, cache.device, stream)
+    if v_out is None:
+        v_out = _new(shape, _torch.float16, cache.device, stream)
+    ks = _kv4_rows(k_out, cache, batch, "k_out", here)
+    vs = _kv4_rows(v_out, cache, batch, "v_out", here)
+    _check(lib().comet_kv4_gather(cache.address, batch.address, k_out.data_ptr(), v_out.data_ptr(),
+                                  ks, vs, _stream(stream)))
+    return k_out, v_out
 
 
 _cus = {}
@@ -791,14 +843,13 @@ def _num_cus(device) -> int:
 
 
 def kv4_attention_workspace(q, cache: KV4Cache, batch: KV4Batch, stream=None):
-    """A workspace tensor for kv4_attention calls of these sizes that do not overlap (None
-    where none is needed)."""
+    """A workspace tensor for kv4_attention calls of these sizes that do not overlap (an empty
+    one where none is needed)."""
     import torch
 
-    n = lib().comet_kv4_attention_workspace(ctypes.addressof(cache.struct),
-                                            ctypes.addressof(batch.struct), q.shape[1],
+    n = lib().comet_kv4_attention_workspace(cache.address, batch.address, q.shape[1],
                                             _num_cus(cache.device))
-    return _new(n, torch.uint8, cache.device, stream) if n else None
+    return _new(n, torch.uint8, cache.device, stream)
 
 
 def kv4_attention(q, cache: KV4Cache, batch: KV4Batch, scale: Optional[float] = None,
@@ -807,29 +858,26 @@ def kv4_attention(q, cache: KV4Cache, batch: KV4Batch, scale: Optional[float] = 
     a wider buffer) over the cache, which holds their own tokens already.  scale defaults to
     head_dim ** -0.5; workspace (of ``kv4_attention_workspace``) is allocated when not given.
     Returns out; rows in no sequence are left as they are (uninitialized in a new tensor)."""
-    import torch
-
-    M, H, D, qs = _heads_of(q, "q")
-    if (M, D) != (batch.M, cache.head_dim):
+    here = _kv4_here(cache, batch)
+    M, H, D, qs = _heads_of(q, "q", here)
+    if M != batch.M or D != cache.head_dim:
         raise ValueError(f"q: shape {tuple(q.shape)}, expected "
                          f"({batch.M}, heads, {cache.head_dim})")
     if out is None:
-        out = _new((M, H, D), torch.float16, q.device, stream)
-    oM, oH, oD, os_ = _heads_of(out, "out")
-    if (oM, oH, oD) != (M, H, D):
-        raise ValueError(f"out: shape {tuple(out.shape)}, expected {(M, H, D)}")
+        out = _new((M, H, D), _torch.float16, q.device, stream)
+        os_ = H * D
+    else:
+        oM, oH, oD, os_ = _heads_of(out, "out", here)
+        if oM != M or oH != H or oD != D:
+            raise ValueError(f"out: shape {tuple(out.shape)}, expected {(M, H, D)}")
     if workspace is None:
         workspace = kv4_attention_workspace(q, cache, batch, stream)
     else:
-        _tensor(workspace, "uint8", "workspace")
-        _on_current(("workspace", workspace.get_device()))
-    _on_current(("q", q.get_device()), ("cache", cache.device.index),
-                ("batch", batch.device.index), ("out", out.get_device()))
+        _plain(workspace, "uint8", "workspace", here)
     _check(lib().comet_kv4_attention(
-        ctypes.addressof(cache.struct), ctypes.addressof(batch.struct), q.data_ptr(),
-        out.data_ptr(), H, qs, os_, D ** -0.5 if scale is None else scale, window,
-        None if workspace is None else workspace.data_ptr(),
-        0 if workspace is None else workspace.numel(), _stream(stream)))
+        cache.address, batch.address, q.data_ptr(), out.data_ptr(), H, qs, os_,
+        D ** -0.5 if scale is None else scale, window, workspace.data_ptr(), workspace.numel(),
+        _stream(stream)))
     return out
 
 

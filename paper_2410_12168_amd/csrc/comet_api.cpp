@@ -790,8 +790,8 @@ comet_status_t comet_kv4_dequantize(const uint8_t* codes, const uint16_t* params
 comet_status_t comet_rope(const uint16_t* X, const int32_t* positions, const double* freqs,
                           uint16_t* out, int M, int heads, int head_dim, int rot_dim, int x_stride,
                           int out_stride, int interleaved, float mscale, hipStream_t stream) {
-  if (!X || !positions || !freqs || !out) return fail(COMET_ERR_INVALID_ARG, "null pointer");
   if (M < 1 || heads < 1) return fail(COMET_ERR_INVALID_ARG, "M=%d, heads=%d must be >= 1", M, heads);
+  if (!X || !positions || !freqs || !out) return fail(COMET_ERR_INVALID_ARG, "null pointer");
   if (M > kMaxQuantRows || heads > 65535)
     return fail(COMET_ERR_UNSUPPORTED, "M=%d, heads=%d exceed %d rows or 65535 heads", M, heads,
                 kMaxQuantRows);
