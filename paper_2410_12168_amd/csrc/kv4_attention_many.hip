@@ -48,10 +48,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
   constexpr int ROW = D / 2;  // bytes of a row of codes
   constexpr int KD = D / 32;  // dwords of codes that a thread turns into fp16
   constexpr int F = 2 * D;    // bytes of a row of fp16
-  constexpr int PARAMS = 4 * NG * kTile;  // [NG][K's s, mn, V's s, mn][64]
-  // of each of the two buffers: K, V, parameters
-  constexpr int V_AT = kTile * F, P_AT = 2 * kTile * F, BUF = P_AT + 4 * PARAMS;
-  __shared__ __attribute__((aligned(16))) uint8_t lds[2 * BUF];
+  constexpr int PARAMS = 3 * NG * kTile;  // [NG][K's s, V's s, mn][64]
+  // of each of the two buffers: K, V, K's offsets (rows of 16 fp16), parameters
+  constexpr int V_AT = kTile * F, M_AT = 2 * kTile * F, P_AT = M_AT + kTile * 32;
+  constexpr int BUF = P_AT + 4 * PARAMS;
+  static_assert(BUF % 256 == 0, "chunks of a row change places within 256 bytes");
+  __shared__ __attribute__((aligned(256))) uint8_t lds[2 * BUF];
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, half = lane >> 5;
@@ -103,7 +105,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
   if (big > 0.0f && big < INFINITY) e = ilogbf(big);
   const float qf = ldexpf(a.scale < 0.0f ? -1.0f : 1.0f, 10 - e);
   // above 0, so that an unseen token's -infinity stays one
-  const float kappa = fmaxf(ldexpf(fabsf(a.scale) * kLog2e, 24 + e - 10), 0x1p-120f);
+  const float kappa = fmaxf(ldexpf(fabsf(a.scale) * kLog2e, 8 + e - 10), 0x1p-120f);
   #pragma unroll
   for (int g = 0; g < NG; ++g) qsum[g] = offset[g] = 0.0f;
   #pragma unroll
@@ -122,15 +124,38 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
                  (_Float16)v[2],            (_Float16)v[6],
                  (_Float16)(v[3] * 0.0625f), (_Float16)(v[7] * 0.0625f)};
   }
-  #pragma unroll
-  for (int g = 0; g < NG; ++g) qsum[g] = pair_sum(qsum[g]) * 0x1p-24f;
+  // The offsets' part of a score, sum_g mn_g (sum q)_g, is a step of the score product
+  // of its own: three fp16 numbers that add up to (sum q)_g * 2^-8 (2^-34 of the row's
+  // largest value off at most), each against mn_g.
+  f16x8 qsums;
+  {
+    f16x8 low = {0, 0, 0, 0, 0, 0, 0, 0}, high = low;  // of the halves of the lanes
+    #pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      float rest = pair_sum(qsum[g]) * 0x1p-8f;
+      #pragma unroll
+      for (int i = 3 * g; i < 3 * g + 3; ++i) {
+        const _Float16 part = (_Float16)rest;
+        rest -= (float)part;
+        if (i < 8)
+          low[i % 8] = part;
+        else
+          high[i % 8] = part;
+      }
+    }
+    const u32x4 lo = __builtin_bit_cast(u32x4, low), hi = __builtin_bit_cast(u32x4, high);
+    u32x4 mine;
+    #pragma unroll
+    for (int i = 0; i < 4; ++i) mine[i] = half ? hi[i] : lo[i];
+    qsums = __builtin_bit_cast(f16x8, mine);
+  }
   float top = kNone, weight_sum = 0.0f;
   f32x16 o[DT];
   #pragma unroll
   for (int d = 0; d < DT; ++d)
     #pragma unroll
     for (int k = 0; k < 16; ++k) o[d][k] = 0.0f;
-  int vexp = -24;  // exponent of the largest scale of V so far, the same in all waves
+  int vexp = -24;  // the exponent below that `o` goes by
 
   // ---- pages: lane 4 i + k has the one of granule k (16 tokens) of the i-th next
   // tile, or -1
@@ -189,56 +214,70 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
     return t * F + 16 * (chunk ^ turn);
   };
 
-  // ---- the loaded tile into LDS; returns the exponent of the scale of the weights
+  // ---- the loaded tile into LDS.  The scale of the weights follows the largest scale
+  // of V so far, 2^exponent or more below 2^(exponent + 1): `limit` is that as fp16 bits.
+  const int k_to = k_place(token, KD * quarter), v_to = V_AT + v_place(token, KD * quarter);
+  int exponent = -24;
+  uint32_t limit = 2;
+  float weight_unit = ldexpf(1.0f, 14 - exponent);
   unsigned long long poison_next = 0;
-  auto stage = [&](int buf, int exponent) {
-    #pragma unroll
-    for (int i = 0; i < KD; ++i) {
-      *reinterpret_cast<f16x8*>(lds + buf + k_place(token, KD * quarter + i)) =
-          codes_f16(kreg[i]);
-      *reinterpret_cast<f16x8*>(lds + buf + V_AT + v_place(token, KD * quarter + i)) =
-          codes_f16(vreg[i]);
-    }
+  // codes: 2 KD pieces, K's and V's in turn
+  auto stage_codes = [&](int buf, int piece) {
+    const int to = piece & 1 ? v_to : k_to, i = piece / 2;
+    *reinterpret_cast<f16x8*>(lds + (buf + to ^ 16 * i)) =
+        codes_f16(piece & 1 ? vreg[i] : kreg[i]);
+  };
+  auto stage_params = [&](int buf) {
     const bool stored = held >> lane & 1;
-    bool bad = false;
+    uint32_t bits = 0, wild = 0;
     #pragma unroll
     for (int g = 0; g < NG; ++g) {
       preg[0][g] = stored ? preg[0][g] : 0u;
       preg[1][g] = stored ? preg[1][g] : 0u;
-      bad |= not_finite(preg[0][g]) || not_finite(preg[1][g]);
+      bits = max(bits, preg[1][g] & 0xFFFFu);
+      // an exponent of all ones carries into the sign
+      wild |= (preg[0][g] & 0x7C007C00u) + 0x04000400u;
+      wild |= (preg[1][g] & 0x7C007C00u) + 0x04000400u;
     }
     // tokens that are not finite make the rows that see them not-a-number, and no
     // others: they count as zeros in the products
+    const bool bad = wild & 0x80008000u;
     poison_next = __ballot(bad);
-    uint32_t bits = 0;
-    #pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      preg[0][g] = bad ? 0u : preg[0][g];
-      preg[1][g] = bad ? 0u : preg[1][g];
-      bits = max(bits, preg[1][g] & 0xFFFFu);
-    }
-    const float vbig = low_half(bits);
-    if (__any(vbig >= ldexpf(1.0f, exponent + 1))) {
-      float m = vbig;
+    if (poison_next) {
+      bits = bad ? 0u : bits;
       #pragma unroll
-      for (int s = 1; s < 64; s <<= 1) m = fmaxf(m, __shfl_xor(m, s));
-      exponent = __builtin_amdgcn_readfirstlane(ilogbf(m));
+      for (int g = 0; g < NG; ++g) {
+        preg[0][g] = bad ? 0u : preg[0][g];
+        preg[1][g] = bad ? 0u : preg[1][g];
+      }
+    }
+    if (__any(bits >= limit)) {
+      uint32_t m = bits;
+      #pragma unroll
+      for (int s = 1; s < 64; s <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, s));
+      exponent = __builtin_amdgcn_readfirstlane(ilogbf(low_half(m)));
+      limit = exponent >= -15 ? (uint32_t)(exponent + 16) << 10 : 1u << (exponent + 25);
+      weight_unit = ldexpf(1.0f, 14 - exponent);
     }
     // the waves take turns at the parameters, which all of them have
-    const float unit_w = ldexpf(1.0f, 14 - exponent);
+    float* at = reinterpret_cast<float*>(lds + buf + P_AT) + lane;
     #pragma unroll
     for (int g = 0; g < NG; ++g) {
-      float* at = reinterpret_cast<float*>(lds + buf + P_AT) + 4 * g * kTile + lane;
-      if (wave == (2 * g & 3)) {
-        at[0] = low_half(preg[0][g]);
-        at[kTile] = low_half(preg[0][g] >> 16);
-      }
-      if (wave == (2 * g + 1 & 3)) {
-        at[2 * kTile] = low_half(preg[1][g]) * unit_w;
-        at[3 * kTile] = low_half(preg[1][g] >> 16);
+      if (wave == 0) at[3 * g * kTile] = low_half(preg[0][g]) * 65536.0f;
+      if (wave == 1) at[(3 * g + 1) * kTile] = low_half(preg[1][g]) * weight_unit;
+      if (wave == 2) at[(3 * g + 2) * kTile] = low_half(preg[1][g] >> 16);
+    }
+    if (wave == 3) {
+      uint32_t* m = reinterpret_cast<uint32_t*>(lds + buf + M_AT + 32 * lane);
+      uint32_t mn[NG];
+      #pragma unroll
+      for (int g = 0; g < NG; ++g) mn[g] = preg[0][g] >> 16;
+      #pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int g0 = 2 * i / 3, g1 = (2 * i + 1) / 3;
+        m[i] = (g0 < NG ? mn[g0 % NG] : 0) | (g1 < NG ? mn[g1 % NG] << 16 : 0);
       }
     }
-    return exponent;
   };
 
   // ---- 32 rows of q times a tile
@@ -252,49 +291,65 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
     const int t0 = tile * kTile;
     const float* params = reinterpret_cast<const float*>(lds + buf + P_AT);
     if (poison && seen_tokens(pos, t0, u.window, poison)) weight_sum = NAN;
+    // The order below is the intended one: next to each product stand the reads of a
+    // later one and other arithmetic, which run while the matrix core works (the
+    // next tile's codes, the first half's scores).
+    constexpr int AHEAD = NG == 1 ? 8 : 4;  // operands of K that are read ahead
     f32x16 x[2];
-    f16x8 k[KS];
-    const uint8_t* k_row = lds + buf;
+    f16x8 k[AHEAD], mn;
+    auto k_operand = [&](int n) {  // of the n-th step, over both halves of the tile
+      return *reinterpret_cast<const f16x8*>(lds + (buf + k_at ^ 32 * (n % KS)) + n / KS * 32 * F);
+    };
+    auto mn_operand = [&](int t) {
+      return *reinterpret_cast<const f16x8*>(lds + buf + M_AT + 32 * (32 * t + col) + 16 * half);
+    };
+    mn = mn_operand(0);
     #pragma unroll
-    for (int s = 0; s < KS; ++s)
-      k[s] = *reinterpret_cast<const f16x8*>(k_row + (k_at ^ 32 * s));
+    for (int n = 0; n < AHEAD; ++n) k[n] = k_operand(n);
+    f32x16 zero;
+    #pragma unroll
+    for (int i = 0; i < 16; ++i) zero[i] = 0.0f;
     #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      __builtin_amdgcn_sched_barrier(0);  // the reads above all come first
+      __builtin_amdgcn_sched_barrier(0);
+      x[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(mn, qsums, zero, 0, 0, 0);
+      if (t == 0) mn = mn_operand(1);
       #pragma unroll
       for (int g = 0; g < NG; ++g) {
-        f32x16 dot;
-        #pragma unroll
-        for (int i = 0; i < 16; ++i) dot[i] = 0.0f;
+        f32x16 d = zero;
         #pragma unroll
         for (int s = g * KS / NG; s < (g + 1) * KS / NG; ++s) {
-          dot = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[s], q[s], dot, 0, 0, 0);
-          if (t == 0)
-            k[s] = *reinterpret_cast<const f16x8*>(k_row + (k_at ^ 32 * s) + 32 * F);
+          const int n = t * KS + s;
+          d = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[n % AHEAD], q[s], d, 0, 0, 0);
+          if (n + AHEAD < 2 * KS) k[n % AHEAD] = k_operand(n + AHEAD);
+          if (n % 2 == 0) {
+            #pragma unroll
+            for (int i = n / 2 * 2 * KD / KS; i < (n / 2 + 1) * 2 * KD / KS; ++i)
+              stage_codes(BUF - buf, i);
+          }
+          __builtin_amdgcn_sched_barrier(0);
         }
         #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float* at = params + 4 * g * kTile + 32 * t + 8 * i + 4 * half;
-          const f32x4 s = *reinterpret_cast<const f32x4*>(at);
-          const f32x4 mn = *reinterpret_cast<const f32x4*>(at + kTile);
+          const f32x4 scale = *reinterpret_cast<const f32x4*>(params + 3 * g * kTile + 32 * t +
+                                                              8 * i + 4 * half);
           #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const float rest = g ? fmaf(mn[r], qsum[g], x[t][4 * i + r]) : mn[r] * qsum[g];
-            x[t][4 * i + r] = fmaf(s[r], dot[4 * i + r], rest);
-          }
+          for (int r = 0; r < 4; ++r)
+            x[t][4 * i + r] = fmaf(scale[r], d[4 * i + r], x[t][4 * i + r]);
         }
+        // done here (see kv4_attention.hip); with one group the scheduler may put the
+        // first half's off until the second's products run
+        if (NG > 1 || t == 1) asm volatile("" : "+v"(x[t]));
       }
     }
-    #pragma unroll
-    for (int t = 0; t < 2; ++t) asm volatile("" : "+v"(x[t]));  // see kv4_attention.hip
+    if (NG == 1) asm volatile("" : "+v"(x[0]));
     // V's operand for 16 tokens of a 32-channel tile
-    const uint8_t* v_row = lds + buf;
     auto v_operand = [&](int st, int d) {
       i16x4 v[2];
       #pragma unroll
       for (int i = 0; i < 2; ++i) {
         v[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (__attribute__((address_space(3))) i16x4*)(v_row + (v_at ^ 64 * d + 32 * i) +
+            (__attribute__((address_space(3))) i16x4*)(lds + (buf + v_at ^ 64 * d + 32 * i) +
                                                        (16 * st + 8 * i) * F));
       }
       return __builtin_bit_cast(f16x8,
@@ -328,78 +383,96 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
       #pragma unroll
       for (int d = 0; d < DT; ++d) o[d] *= f;
     }
-    #pragma unroll
-    for (int t = 0; t < 2; ++t)
+    // the weighted sum, 16 tokens at a time; the weights of the next 16 are worked out
+    // next to the products of these
+    auto weights = [&](int st, int i) {  // of tokens 8 i + 4 half .. + 3 of the 16
       #pragma unroll
-      for (int k = 0; k < 16; ++k) {
-        const float p = __builtin_amdgcn_exp2f(fmaf(x[t][k], kappa, -top));
-        x[t][k] = p;
-        weight_sum += p;
+      for (int r = 0; r < 4; ++r) {
+        const int k = 8 * (st & 1) + 4 * i + r;
+        const float wt = __builtin_amdgcn_exp2f(fmaf(x[st / 2][k], kappa, -top));
+        x[st / 2][k] = wt;
+        weight_sum += wt;
       }
-    // the weighted sum, 16 tokens at a time
+    };
+    auto operand = [&](int st, int g) {
+      f16x8 p;
+      #pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float* at = params + (3 * g + 1) * kTile + 16 * st + 8 * i + 4 * half;
+        const f32x4 s = *reinterpret_cast<const f32x4*>(at);
+        const f32x4 m = *reinterpret_cast<const f32x4*>(at + kTile);
+        #pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float wt = x[st / 2][8 * (st & 1) + 4 * i + r];
+          offset[g] = fmaf(wt, m[r], offset[g]);
+          p[4 * i + r] = (_Float16)(wt * s[r]);
+        }
+      }
+      return p;
+    };
+    weights(0, 0);
+    weights(0, 1);
+    f16x8 p = operand(0, 0);
     #pragma unroll
     for (int st = 0; st < 4; ++st) {
       #pragma unroll
       for (int g = 0; g < NG; ++g) {
-        f16x8 p;
-        #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const float* at = params + (4 * g + 2) * kTile + 16 * st + 8 * i + 4 * half;
-          const f32x4 s = *reinterpret_cast<const f32x4*>(at);
-          const f32x4 mn = *reinterpret_cast<const f32x4*>(at + kTile);
-          #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const float wt = x[st / 2][8 * (st & 1) + 4 * i + r];
-            offset[g] = fmaf(wt, mn[r], offset[g]);
-            p[4 * i + r] = (_Float16)(wt * s[r]);
-          }
-        }
+        f16x8 p_next = p;
         #pragma unroll
         for (int d = g * DT / NG; d < (g + 1) * DT / NG; ++d) {
+          __builtin_amdgcn_sched_barrier(0);
           o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[d], p, o[d], 0, 0, 0);
-          if (st < 3) v[d] = v_operand(st + 1, d);
+          if (st < 3) {
+            v[d] = v_operand(st + 1, d);
+            if (d % (DT / 2) == 0) weights(st + 1, d / (DT / 2));
+          }
         }
+        // the next operand: the next group's, or the first of the next 16 tokens
+        if (g + 1 < NG)
+          p_next = operand(st, g + 1);
+        else if (st < 3)
+          p_next = operand(st + 1, 0);
+        p = p_next;
       }
-      __builtin_amdgcn_sched_barrier(0);
     }
   };
 
   if (tile0 < tile1) {
     load_pages(tile0);
     load(tile0, 0);
-    int exponent = stage(0, vexp);
+    stage_params(0);
+    #pragma unroll
+    for (int i = 0; i < 2 * KD; ++i) stage_codes(0, i);
+    int exponent_now = exponent;  // of the tile in work
     unsigned long long have = held, poison = poison_next;
     if (tile0 + 1 < tile1) load(tile0 + 1, 1);
     int ahead = 1;  // where in `pages` the loaded tile is
     for (int tile = tile0; tile < tile1; ++tile) {
-      const int buf = (tile - tile0) & 1 ? BUF : 0;
+      int buf = (tile - tile0) & 1 ? BUF : 0;
+      // worked out anew for each tile: the addresses of both buffers would take the
+      // registers of q
+      asm volatile("" : "+s"(buf));
       __syncthreads();  // the tile is in LDS, and the other buffer is free
-      int exponent_next = exponent;
-      unsigned long long have_next = 0;
-      if (tile + 1 < tile1) {
-        exponent_next = stage(BUF - buf, exponent);
-        have_next = held;
-        if (tile + 2 < tile1) {
-          if (++ahead == 16) {
-            load_pages(tile + 2);
-            ahead = 0;
-          }
-          load(tile + 2, ahead);
-        }
+      // the next tile is staged on the way (after the last one, once more to no end)
+      if (tile + 1 < tile1) stage_params(BUF - buf);
+      const unsigned long long have_next = held;
+      // a wave whose rows see nothing of the tile works on it like the others: a second
+      // path for it would cost the first one its registers
+      if (exponent_now != vexp) {
+        const float f = ldexpf(1.0f, vexp - exponent_now);
+        vexp = exponent_now;
+        #pragma unroll
+        for (int d = 0; d < DT; ++d) o[d] *= f;
       }
-      const int t0 = tile * kTile;
-      const bool some = wave_rows > 0 && t0 <= wave_pos1 &&
-                        (u.window == 0 || t0 + kTile - 1 > wave_pos0 - u.window);
-      if (some) {
-        if (exponent != vexp) {
-          const float f = ldexpf(1.0f, vexp - exponent);
-          vexp = exponent;
-          #pragma unroll
-          for (int d = 0; d < DT; ++d) o[d] *= f;
+      work(buf, tile, have, poison);
+      if (tile + 2 < tile1) {
+        if (++ahead == 16) {
+          load_pages(tile + 2);
+          ahead = 0;
         }
-        work(buf, tile, have, poison);
+        load(tile + 2, ahead);
       }
-      exponent = exponent_next;
+      exponent_now = exponent;
       have = have_next;
       poison = poison_next;
     }
