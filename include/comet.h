@@ -274,8 +274,8 @@ COMET_API comet_status_t comet_rope_frequencies(double* freqs, int rot_dim, doub
  * comet_kv4_quantize gives it (groups of G channels), so comet_kv4_dequantize
  * reads pages with T = rows, C = head_dim.
  * page_size a power of two, 16 .. 1024; head_dim 64 or 128; G 32, 64 or 128, at
- * most head_dim; kv_heads at most 1024; num_pages >= 1 (any number that fits the
- * memory).  All four buffers 16-byte aligned. */
+ * most head_dim; kv_heads at most 1024; num_pages * kv_heads below 2^31.
+ * All four buffers 16-byte aligned. */
 typedef struct {
   uint8_t* k_codes;
   uint16_t* k_params;

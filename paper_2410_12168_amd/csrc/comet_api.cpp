@@ -592,6 +592,9 @@ comet_status_t check_cache(const comet_kv4_cache_t* c, bool buffers, comet::Page
                 c->kv_heads);
   if (c->kv_heads > 1024)
     return fail(COMET_ERR_UNSUPPORTED, "kv_heads=%d exceeds 1024", c->kv_heads);
+  if ((long long)c->num_pages * c->kv_heads > INT32_MAX)
+    return fail(COMET_ERR_UNSUPPORTED, "num_pages=%d times kv_heads=%d exceeds 2^31 - 1",
+                c->num_pages, c->kv_heads);
   if (buffers) {
     if (!c->k_codes || !c->k_params || !c->v_codes || !c->v_params)
       return fail(COMET_ERR_INVALID_ARG, "null pointer in the cache");

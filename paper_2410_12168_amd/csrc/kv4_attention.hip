@@ -153,21 +153,27 @@ __global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_few
   uint8_t* stage = lds + wave * STAGE;
   float* params = reinterpret_cast<float*>(stage + kTile * ROW);
 
-  // ---- pages: lane 4 i + k has the one of granule k (16 tokens) of this wave's i-th
-  // next tile, or -1, so that a tile's pages are scalars and its loads do not wait
-  // behind a load of the table
+  // ---- pages: lane 4 i + k has the slab (page and head) of granule k (16 tokens) of
+  // this wave's i-th next tile, or -1, so that a tile's slabs are scalars and its loads
+  // do not wait behind a load of the table
   const int32_t* table = b.block_table + (long long)unit.seq * b.max_pages;
-  int pages = -1;
+  const bool one_page = c.page_shift >= 6;  // a tile lies in one
+  int slabs = -1;
   auto load_pages = [&](int tile) {
     const int token = (tile + (lane >> 2) * kWaves) * kTile + 16 * (lane & 3);
     const int i = token >> c.page_shift;
-    const int page = i < b.max_pages ? table[i] : -1;
-    pages = (unsigned)page < (unsigned)c.num_pages ? page : -1;
+    slabs = slab_of(c, head, i < b.max_pages ? table[i] : -1);
   };
-  auto page_of = [&](int i, int k) { return __builtin_amdgcn_readlane(pages, 4 * i + k); };
-  // first row of granule k's 16 in the cache; a hole reads page 0
-  auto granule_row = [&](int tile, int i, int k) -> long long {
-    return cache_row(c, max(page_of(i, k), 0), head, tile * kTile + 16 * k);
+  // First rows in the cache of the tile's granules; a hole reads the first page.
+  auto granule_rows = [&](int tile, int i, long long (&rows4)[4]) {
+    rows4[0] = slab_row(c, __builtin_amdgcn_readlane(slabs, 4 * i), tile * kTile);
+    #pragma unroll
+    for (int k = 1; k < 4; ++k) rows4[k] = rows4[0] + 16 * k;
+    if (!one_page) {
+      #pragma unroll
+      for (int k = 1; k < 4; ++k)
+        rows4[k] = slab_row(c, __builtin_amdgcn_readlane(slabs, 4 * i + k), tile * kTile + 16 * k);
+    }
   };
 
   // ---- loads of a tile: into registers, a tile ahead
@@ -176,10 +182,11 @@ __global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_few
   uint32_t preg[2][NG];
   unsigned long long held = 0;  // tokens that are in the cache
   auto load_k = [&](int tile, int ahead) {
+    long long rows4[4];
+    granule_rows(tile, ahead, rows4);
     #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const uint8_t* at =
-          c.k_codes + granule_row(tile, ahead, j) * ROW + (unsigned)(col * ROW + ROW / 4 * quad);
+      const uint8_t* at = c.k_codes + rows4[j] * ROW + (unsigned)(col * ROW + ROW / 4 * quad);
       if constexpr (KS == 4) {
         const u32x4 v = *reinterpret_cast<const u32x4*>(at);
         kreg[j][0] = v[0], kreg[j][1] = v[1], kreg[j][2] = v[2], kreg[j][3] = v[3];
@@ -191,8 +198,7 @@ __global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_few
   };
   auto load_v = [&](int tile, int ahead) {
     long long rows4[4];
-    #pragma unroll
-    for (int k = 0; k < 4; ++k) rows4[k] = granule_row(tile, ahead, k);
+    granule_rows(tile, ahead, rows4);
     #pragma unroll
     for (int i = 0; i < VL; ++i) {
       if constexpr (VL == 4) {
@@ -213,7 +219,7 @@ __global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_few
     held = 0;
     #pragma unroll
     for (int k = 0; k < 4; ++k)
-      if (page_of(ahead, k) >= 0) held |= 0xFFFFull << (16 * k);
+      if (__builtin_amdgcn_readlane(slabs, 4 * ahead + k) >= 0) held |= 0xFFFFull << (16 * k);
     const int left = w.len - tile * kTile;
     if (left < kTile) held &= (1ull << max(left, 0)) - 1;
   };
@@ -315,6 +321,8 @@ __global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_few
           x[cb][j][r] = p;
           weight_sum[cb] += p;
         }
+    #pragma unroll
+    for (int cb = 0; cb < C; ++cb) asm volatile("" : "+v"(weight_sum[cb]));
     // the weighted sum, group by group
     #pragma unroll
     for (int g = 0; g < NG; ++g) {
@@ -332,6 +340,8 @@ __global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_few
             offset[cb][g] = fmaf(x[cb][j][r], mn[r], offset[cb][g]);
             p[cb][j / 2][2 * r + j % 2] = (_Float16)(x[cb][j][r] * s[r]);
           }
+        #pragma unroll
+        for (int cb = 0; cb < C; ++cb) asm volatile("" : "+v"(offset[cb][g]));
       }
       #pragma unroll
       for (int d = g * DB / NG; d < (g + 1) * DB / NG; ++d) {

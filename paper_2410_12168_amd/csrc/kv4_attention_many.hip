@@ -157,14 +157,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
     for (int k = 0; k < 16; ++k) o[d][k] = 0.0f;
   int vexp = -24;  // the exponent below that `o` goes by
 
-  // ---- pages: lane 4 i + k has the one of granule k (16 tokens) of the i-th next
-  // tile, or -1
+  // ---- pages: lane 4 i + k has the slab (page and head) of granule k (16 tokens) of
+  // the i-th next tile, or -1
   const int32_t* table = b.block_table + (long long)unit.seq * b.max_pages;
-  int pages = -1;
+  const bool one_page = c.page_shift >= 6;  // a tile lies in one
+  int slabs = -1;
   auto load_pages = [&](int tile) {
     const int i = (tile * kTile + 16 * lane) >> c.page_shift;
-    const int page = i < b.max_pages ? table[i] : -1;
-    pages = (unsigned)page < (unsigned)c.num_pages ? page : -1;
+    slabs = slab_of(c, head, i < b.max_pages ? table[i] : -1);
   };
   // ---- loads of a tile: a thread takes a quarter of the codes of one token of its
   // wave's granule, and the parameters of token `lane`
@@ -172,11 +172,26 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
   uint32_t kreg[KD], vreg[KD], preg[2][NG];
   unsigned long long held = 0;  // tokens that are in the cache
   auto load = [&](int tile, int ahead) {
-    auto row_of = [&](int k) {
-      const int page = __builtin_amdgcn_readlane(pages, 4 * ahead + k);
-      return cache_row(c, max(page, 0), head, tile * kTile + 16 * k);
-    };
-    const long long row = row_of(wave);
+    const int t = tile * kTile;
+    int slab[4];
+    slab[0] = __builtin_amdgcn_readlane(slabs, 4 * ahead);
+    long long row = slab_row(c, slab[0], t), mine = row + (lane & 48);
+    row += 16 * wave;
+    held = slab[0] >= 0 ? ~0ull : 0;
+    if (!one_page) {
+      #pragma unroll
+      for (int k = 1; k < 4; ++k) slab[k] = __builtin_amdgcn_readlane(slabs, 4 * ahead + k);
+      row = slab_row(c, wave < 2 ? (wave ? slab[1] : slab[0]) : (wave == 2 ? slab[2] : slab[3]),
+                     t + 16 * wave);
+      mine = slab_row(c, quarter < 2 ? (quarter ? slab[1] : slab[0])
+                                     : (quarter == 2 ? slab[2] : slab[3]), t + 16 * quarter);
+      held = 0;
+      #pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (slab[k] >= 0) held |= 0xFFFFull << (16 * k);
+    }
+    const int left = w.len - t;
+    if (left < kTile) held &= (1ull << max(left, 0)) - 1;
     const unsigned at = (lane & 15) * ROW + ROW / 4 * quarter;
     if constexpr (KD == 4) {
       const u32x4 k = *reinterpret_cast<const u32x4*>(c.k_codes + row * ROW + at);
@@ -189,20 +204,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
       #pragma unroll
       for (int i = 0; i < 2; ++i) kreg[i] = k[i], vreg[i] = v[i];
     }
-    const long long r0 = row_of(0), r1 = row_of(1), r2 = row_of(2), r3 = row_of(3);
-    const long long mine = quarter < 2 ? (quarter == 0 ? r0 : r1) : (quarter == 2 ? r2 : r3);
     const long long p = (mine + (lane & 15)) * NG;
     #pragma unroll
     for (int g = 0; g < NG; ++g) {
       preg[0][g] = reinterpret_cast<const uint32_t*>(c.k_params)[p + g];
       preg[1][g] = reinterpret_cast<const uint32_t*>(c.v_params)[p + g];
     }
-    held = 0;
-    #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (__builtin_amdgcn_readlane(pages, 4 * ahead + k) >= 0) held |= 0xFFFFull << (16 * k);
-    const int left = w.len - tile * kTile;
-    if (left < kTile) held &= (1ull << max(left, 0)) - 1;
   };
 
   // Where a 16-byte chunk (8 channels) of a token lies in LDS.
@@ -393,6 +400,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
         x[st / 2][k] = wt;
         weight_sum += wt;
       }
+      asm volatile("" : "+v"(weight_sum));  // here and not after the products
     };
     auto operand = [&](int st, int g) {
       f16x8 p;
@@ -408,8 +416,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
           p[4 * i + r] = (_Float16)(wt * s[r]);
         }
       }
+      asm volatile("" : "+v"(offset[g]));
       return p;
     };
+    __builtin_amdgcn_s_setprio(1);  // the part with most products first
     weights(0, 0);
     weights(0, 1);
     f16x8 p = operand(0, 0);
@@ -435,6 +445,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
         p = p_next;
       }
     }
+    __builtin_amdgcn_s_setprio(0);
   };
 
   if (tile0 < tile1) {

@@ -19,6 +19,18 @@ __device__ inline int token_page(const PagedBatch& b, int seq, long long pos, in
   return (unsigned)page < (unsigned)num_pages ? page : -1;
 }
 
+// A slab is the part of a page that one head has: page * kv_heads + head, below
+// 2^31 (the interface refuses larger caches).  -1 for a page outside the cache.
+__device__ inline int slab_of(const PagedCache& c, int head, int page) {
+  return (unsigned)page < (unsigned)c.num_pages ? page * c.kv_heads + head : -1;
+}
+
+// Row of token `pos` in its slab among all rows of the cache; a hole reads the
+// first slab.
+__device__ inline long long slab_row(const PagedCache& c, int slab, int pos) {
+  return ((long long)max(slab, 0) << c.page_shift) + (pos & ((1 << c.page_shift) - 1));
+}
+
 // Row of (page, head, slot) among all rows of the cache; pages of a long cache
 // pass 32 bits.
 __device__ inline long long cache_row(const PagedCache& c, int page, int head, long long pos) {
