@@ -150,36 +150,33 @@ __device__ inline T from_lane(T v, int at) {
   return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), at));
 }
 
-// Tiles of a range at most, from the work of all sequences: the same in every wave
-// of a launch.  Rounded up by more than the 32-bit sum can be off, so that the
-// ranges of full length are `target` at most.
-__device__ inline float tiles_per_range(const PagedBatch& b, int page_shift, const UnitShape& u) {
-  const int lane = threadIdx.x & 63;
-  float total = 0.0f;
-  for (int s = 0; s < b.B; s += 64) {
-    const SeqWork w = seq_work(b, page_shift, u, s + lane);
-    total += (float)w.blocks * (float)w.tiles;
-  }
-  total = from_lane(sum_upto(total), 63) * 1.001f;
-  return fmaxf((float)kMinTiles, ceilf(total / (float)u.target));
-}
-
 __device__ inline uint32_t ranges_of(const SeqWork& w, float per) {
   return (uint32_t)ceilf((float)w.tiles / per);
 }
 
 // Unit `index`, counted over sequences, row blocks and ranges (SPLIT: row block
 // `index` of those whose sequence has more than one range).  False if there is
-// none.  Sums of 32 bits: more than a launch can have only in batches that the
-// interface does not allow, whose units are then any or none of the batch's.
+// none.  Every wave of a launch works out the same from the lengths of all
+// sequences, 64 at a time: first how many tiles a range may have, so that the
+// ranges of full length are `target` at most (rounded up by more than the 32-bit
+// sum can be off), then where the unit is.  Sums of 32 bits: more than a launch
+// can have only in batches that the interface does not allow, whose units are then
+// any or none of the batch's.
 template <bool SPLIT>
 __device__ inline bool find_unit(const PagedBatch& b, int page_shift, const UnitShape& u,
                                  uint32_t index, Unit* out) {
   const int lane = threadIdx.x & 63;
-  const float per = tiles_per_range(b, page_shift, u);
+  const SeqWork start = seq_work(b, page_shift, u, lane);
+  float total = (float)start.blocks * (float)start.tiles;
+  for (int s = 64; s < b.B; s += 64) {
+    const SeqWork w = seq_work(b, page_shift, u, s + lane);
+    total += (float)w.blocks * (float)w.tiles;
+  }
+  total = from_lane(sum_upto(total), 63) * 1.001f;
+  const float per = fmaxf((float)kMinTiles, ceilf(total / (float)u.target));
   uint32_t before = 0, slots_before = 0;
   for (int s = 0; s < b.B; s += 64) {
-    const SeqWork w = seq_work(b, page_shift, u, s + lane);
+    const SeqWork w = s == 0 ? start : seq_work(b, page_shift, u, s + lane);
     const uint32_t ranges = ranges_of(w, per);
     const uint32_t slots = ranges > 1 ? w.blocks * ranges : 0;
     const uint32_t mine = SPLIT ? (ranges > 1 ? w.blocks : 0) : w.blocks * ranges;

@@ -55,7 +55,7 @@ __global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_few
   constexpr int VL = ROW / 16;      // 16-byte loads of V per lane
   // V's codes, then the parameters in 32 bits: [NG][K's s, mn, V's s, mn][64]
   constexpr int STAGE = kTile * ROW + 4 * NG * kTile * 4;
-  constexpr int OPAD = 36;          // floats of a row of 32 sums in LDS
+  constexpr int OPAD = D + 4;       // floats of a row of sums in LDS
   constexpr int SUMS = kWaves * 16 * C * OPAD * 4;
   constexpr int STATS = kWaves * 16 * C * (2 + NG) * 4;
   constexpr int LDS = STAGE * kWaves > SUMS ? STAGE * kWaves : SUMS;
@@ -83,75 +83,6 @@ __global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_few
   else
     tile1 = min(tile1, min(pos1, cap - 1) / kTile + 1);
   if (u.window > 0) tile0 = max(tile0, max(0, pos0 - u.window + 1) / kTile);
-
-  // ---- q: operand [step] of each column block, its sums and factor
-  f16x8 q[C][KS];
-  float qsum[C][NG], kappa[C], top[C], weight_sum[C], offset[C][NG];
-  int pos[C];
-  #pragma unroll
-  for (int cb = 0; cb < C; ++cb) {
-    const int r = 16 * cb + col;
-    const bool live = r < rows;
-    const int i = (row0 + r) / u.group, h = (row0 + r) % u.group;
-    pos[cb] = w.len - w.n + i;
-    const uint16_t* x = a.Q + (long long)(w.start + i) * a.q_stride + (head * u.group + h) * D;
-    u32x4 raw[KS];
-    float big = 0.0f;
-    #pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      // a lane's codes of K: D / 4 channels in a row, or 8 of every 32 where the
-      // steps have to stay within a group (as load_k's rows are turned)
-      const int at = NG == 1 ? D / 4 * quad + 8 * s
-                     : KS == 4 ? 32 * s + 8 * quad
-                               : 32 * s + 16 * (quad & 1) + 8 * (quad >> 1);
-      raw[s] = u32x4{0, 0, 0, 0};
-      if (live) raw[s] = *reinterpret_cast<const u32x4*>(x + at);
-      #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        big = fmaxf(big, fmaxf(fabsf(low_half(raw[s][k])), fabsf(low_half(raw[s][k] >> 16))));
-    }
-    big = quad_max(big);
-    int e = 10;
-    if (big > 0.0f && big < INFINITY) e = ilogbf(big);
-    const float f = ldexpf(a.scale < 0.0f ? -1.0f : 1.0f, 10 - e);
-    // above 0, so that an unseen token's -infinity stays one
-    kappa[cb] = fmaxf(ldexpf(fabsf(a.scale) * kLog2e, 24 + e - 10), 0x1p-120f);
-    #pragma unroll
-    for (int g = 0; g < NG; ++g) qsum[cb][g] = 0.0f;
-    #pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      float v[8];
-      float sum = 0.0f;
-      #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        v[2 * k] = low_half(raw[s][k]) * f;
-        v[2 * k + 1] = low_half(raw[s][k] >> 16) * f;
-        sum += v[2 * k] + v[2 * k + 1];
-      }
-      qsum[cb][32 * s / G % NG] += sum;
-      q[cb][s] = f16x8{(_Float16)v[0],            (_Float16)v[4],
-                       (_Float16)(v[1] * 0.0625f), (_Float16)(v[5] * 0.0625f),
-                       (_Float16)v[2],            (_Float16)v[6],
-                       (_Float16)(v[3] * 0.0625f), (_Float16)(v[7] * 0.0625f)};
-    }
-    #pragma unroll
-    for (int g = 0; g < NG; ++g) qsum[cb][g] = quad_sum(qsum[cb][g]) * 0x1p-24f;
-    top[cb] = kNone;
-    weight_sum[cb] = 0.0f;
-    #pragma unroll
-    for (int g = 0; g < NG; ++g) offset[cb][g] = 0.0f;
-  }
-
-  f32x4 o[C][DB];
-  #pragma unroll
-  for (int cb = 0; cb < C; ++cb)
-    #pragma unroll
-    for (int d = 0; d < DB; ++d) o[cb][d] = f32x4{0, 0, 0, 0};
-  int vexp = -24;  // exponent of the largest scale of V so far
-  float weight_unit = ldexpf(1.0f, (lane & 1 ? 10 : 14) - vexp);
-
-  uint8_t* stage = lds + wave * STAGE;
-  float* params = reinterpret_cast<float*>(stage + kTile * ROW);
 
   // ---- pages: lane 4 i + k has the slab (page and head) of granule k (16 tokens) of
   // this wave's i-th next tile, or -1, so that a tile's slabs are scalars and its loads
@@ -223,6 +154,90 @@ __global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_few
     const int left = w.len - tile * kTile;
     if (left < kTile) held &= (1ull << max(left, 0)) - 1;
   };
+
+  const int first = tile0 + wave;
+  int ahead = 0;  // where in `slabs` the next tile is
+  if (first < tile1) load_pages(first);
+
+  // ---- q: operand [step] of each column block, its sums and factor
+  f16x8 q[C][KS];
+  float qsum[C][NG], kappa[C], top[C], weight_sum[C], offset[C][NG];
+  int pos[C];
+  u32x4 raw_q[C][KS];
+  #pragma unroll
+  for (int cb = 0; cb < C; ++cb) {
+    const int r = 16 * cb + col;
+    const bool live = r < rows;
+    const int i = (row0 + r) / u.group, h = (row0 + r) % u.group;
+    pos[cb] = w.len - w.n + i;
+    const uint16_t* x = a.Q + (long long)(w.start + i) * a.q_stride + (head * u.group + h) * D;
+    #pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      // a lane's codes of K: D / 4 channels in a row, or 8 of every 32 where the
+      // steps have to stay within a group (as load_k's rows are turned)
+      const int at = NG == 1 ? D / 4 * quad + 8 * s
+                     : KS == 4 ? 32 * s + 8 * quad
+                               : 32 * s + 16 * (quad & 1) + 8 * (quad >> 1);
+      raw_q[cb][s] = u32x4{0, 0, 0, 0};
+      if (live) raw_q[cb][s] = *reinterpret_cast<const u32x4*>(x + at);
+    }
+  }
+  if (first < tile1) {
+    load_k(first, 0);
+    load_v(first, 0);
+  }
+  #pragma unroll
+  for (int cb = 0; cb < C; ++cb) {
+    const u32x4 (&raw)[KS] = raw_q[cb];
+    float big = 0.0f;
+    #pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      #pragma unroll
+      for (int k = 0; k < 4; ++k)
+        big = fmaxf(big, fmaxf(fabsf(low_half(raw[s][k])), fabsf(low_half(raw[s][k] >> 16))));
+    }
+    big = quad_max(big);
+    int e = 10;
+    if (big > 0.0f && big < INFINITY) e = ilogbf(big);
+    const float f = ldexpf(a.scale < 0.0f ? -1.0f : 1.0f, 10 - e);
+    // above 0, so that an unseen token's -infinity stays one
+    kappa[cb] = fmaxf(ldexpf(fabsf(a.scale) * kLog2e, 24 + e - 10), 0x1p-120f);
+    #pragma unroll
+    for (int g = 0; g < NG; ++g) qsum[cb][g] = 0.0f;
+    #pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      float v[8];
+      float sum = 0.0f;
+      #pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        v[2 * k] = low_half(raw[s][k]) * f;
+        v[2 * k + 1] = low_half(raw[s][k] >> 16) * f;
+        sum += v[2 * k] + v[2 * k + 1];
+      }
+      qsum[cb][32 * s / G % NG] += sum;
+      q[cb][s] = f16x8{(_Float16)v[0],            (_Float16)v[4],
+                       (_Float16)(v[1] * 0.0625f), (_Float16)(v[5] * 0.0625f),
+                       (_Float16)v[2],            (_Float16)v[6],
+                       (_Float16)(v[3] * 0.0625f), (_Float16)(v[7] * 0.0625f)};
+    }
+    #pragma unroll
+    for (int g = 0; g < NG; ++g) qsum[cb][g] = quad_sum(qsum[cb][g]) * 0x1p-24f;
+    top[cb] = kNone;
+    weight_sum[cb] = 0.0f;
+    #pragma unroll
+    for (int g = 0; g < NG; ++g) offset[cb][g] = 0.0f;
+  }
+
+  f32x4 o[C][DB];
+  #pragma unroll
+  for (int cb = 0; cb < C; ++cb)
+    #pragma unroll
+    for (int d = 0; d < DB; ++d) o[cb][d] = f32x4{0, 0, 0, 0};
+  int vexp = -24;  // exponent of the largest scale of V so far
+  float weight_unit = ldexpf(1.0f, (lane & 1 ? 10 : 14) - vexp);
+
+  uint8_t* stage = lds + wave * STAGE;
+  float* params = reinterpret_cast<float*>(stage + kTile * ROW);
 
   // Where a 16-byte chunk of V's row lies in LDS: the 16 rows of a transposing read
   // (16 j + 4 quad + r, one chunk) in different banks.
@@ -361,13 +376,6 @@ __global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_few
     }
   };
 
-  const int first = tile0 + wave;
-  int ahead = 0;  // where in `pages` the next tile is
-  if (first < tile1) {
-    load_pages(first);
-    load_k(first, 0);
-    load_v(first, 0);
-  }
   for (int tile = first; tile < tile1; tile += kWaves) {
     const unsigned long long have = held;
     const bool stored = have >> lane & 1;
@@ -494,38 +502,36 @@ __global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_few
   }
   float* sums = reinterpret_cast<float*>(lds);  // [wave][16 C][OPAD]
   #pragma unroll
-  for (int d = 0; d < D / 32; ++d) {
-    __syncthreads();
+  for (int cb = 0; cb < C; ++cb)
     #pragma unroll
-    for (int cb = 0; cb < C; ++cb)
-      #pragma unroll
-      for (int k = 0; k < 2; ++k)
-        *reinterpret_cast<f32x4*>(sums + (wave * 16 * C + 16 * cb + col) * OPAD + 16 * k +
-                                  4 * quad) = o[cb][2 * d + k] * factor[cb];
-    __syncthreads();
+    for (int d = 0; d < DB; ++d)
+      *reinterpret_cast<f32x4*>(sums + (wave * 16 * C + 16 * cb + col) * OPAD + 16 * d +
+                                4 * quad) = o[cb][d] * factor[cb];
+  __syncthreads();
+  #pragma unroll
+  for (int cb = 0; cb < C; ++cb) {
+    const int r = 16 * cb + my_row;
+    if (r >= rows) continue;
+    const float f = my_sum[cb] != 0.0f ? 1.0f / my_sum[cb] : 0.0f;
+    const int i = (row0 + r) / u.group, h = (row0 + r) % u.group;
+    uint16_t* out =
+        a.out + (long long)(w.start + i) * a.out_stride + (head * u.group + h) * D + my_channel;
+    const long long at = ((long long)unit.slot * c.kv_heads + head) * u.rows + r;
+    if (unit.ranges > 1 && unit.slot >= part.slots) continue;  // no batch that comet.h allows
     #pragma unroll
-    for (int cb = 0; cb < C; ++cb) {
-      const int r = 16 * cb + my_row;
+    for (int d = 0; d < D / 32; ++d) {
       const float off = my_offset[cb][32 * d / G];
       f32x2 v = {off, off};
       #pragma unroll
       for (int k = 0; k < kWaves; ++k)
-        v += *reinterpret_cast<const f32x2*>(sums + (k * 16 * C + r) * OPAD + my_channel);
-      if (r >= rows) continue;
-      if (unit.ranges > 1) {
-        if (unit.slot >= part.slots) continue;  // no batch that comet.h allows
-        const long long at = ((long long)unit.slot * c.kv_heads + head) * u.rows + r;
+        v += *reinterpret_cast<const f32x2*>(sums + (k * 16 * C + r) * OPAD + 32 * d + my_channel);
+      if (unit.ranges > 1)
         *reinterpret_cast<f32x2*>(part.sums + at * D + 32 * d + my_channel) = v;
-        if (d == 0 && my_channel == 0)
-          *reinterpret_cast<f32x2*>(part.stats + at * 2) = f32x2{my_top[cb], my_sum[cb]};
-      } else {
-        const float f = my_sum[cb] != 0.0f ? 1.0f / my_sum[cb] : 0.0f;
-        const int i = (row0 + r) / u.group, h = (row0 + r) % u.group;
-        const f16x2 y = {(_Float16)(v[0] * f), (_Float16)(v[1] * f)};
-        *reinterpret_cast<f16x2*>(a.out + (long long)(w.start + i) * a.out_stride +
-                                  (head * u.group + h) * D + 32 * d + my_channel) = y;
-      }
+      else
+        *reinterpret_cast<f16x2*>(out + 32 * d) = f16x2{(_Float16)(v[0] * f), (_Float16)(v[1] * f)};
     }
+    if (unit.ranges > 1 && my_channel == 0)
+      *reinterpret_cast<f32x2*>(part.stats + at * 2) = f32x2{my_top[cb], my_sum[cb]};
   }
 }
 
@@ -533,23 +539,22 @@ __global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_few
 // one (grid x: row block and kv head, y: rows).  D / 4 lanes of four channels make a
 // group; a group takes a row, or, the more ranges there are, several take turns at
 // those of one.
-constexpr int kCombineRows = 4;       // of a block, in the kernel for few rows
-constexpr int kCombineManyRows = 32;  // in the other
-constexpr int kAhead = 8;             // ranges that a group has in flight
+constexpr int kAhead = 8;  // ranges that a group has in flight
 
 __global__ __launch_bounds__(256) void kv4_attention_combine_kernel(PagedCache c, PagedBatch b,
                                                                     AttentionArgs a,
                                                                     UnitShape few, Partials few_part,
                                                                     UnitShape many,
                                                                     Partials many_part,
-                                                                    int few_blocks) {
+                                                                    int few_blocks, int few_rows,
+                                                                    int many_rows) {
   __shared__ f32x4 sums[256];
   __shared__ f32x2 stats[256];
   const bool is_few = (int)blockIdx.x < few_blocks;
   const UnitShape u = is_few ? few : many;
   const Partials part = is_few ? few_part : many_part;
   const int index = blockIdx.x - (is_few ? 0 : few_blocks);
-  const int my_rows = is_few ? kCombineRows : kCombineManyRows;
+  const int my_rows = is_few ? few_rows : many_rows;
   if ((int)blockIdx.y * my_rows >= u.rows) return;
   Unit unit;
   if (!find_unit<true>(b, c.page_shift, u, index / c.kv_heads, &unit)) return;
@@ -640,7 +645,8 @@ struct Part {
   UnitShape u;
   long long blocks;  // of the grid: units that a batch of these sizes may have, times kv heads
   long long slots;   // partial results
-  int most_rows;     // of a row block
+  long long row_blocks;
+  int most_rows;     // of one
 };
 
 // `resident`: blocks that a compute unit holds at a time.
@@ -656,6 +662,7 @@ Part part_of(const PagedCache& c, const PagedBatch& b, int heads, int window, in
   p.most_rows = (int)std::min<long long>(rows, (long long)b.max_rows * p.u.group);
   // every sequence's last row block may be ragged
   const long long row_blocks = (long long)b.M * p.u.group / rows + std::min(b.B, b.M);
+  p.row_blocks = row_blocks;
   const long long tiles = (((long long)b.max_pages << c.page_shift) + kTile - 1) / kTile;
   const long long ranges = (tiles + kMinTiles - 1) / kMinTiles;
   p.slots = ranges > 1 ? std::min<long long>(2 * p.u.target, row_blocks * ranges) : 0;
@@ -691,10 +698,22 @@ Partials partials_at(float* at, const PagedCache& c, const Part& p) {
   return {at, at + p.slots * c.kv_heads * p.u.rows * c.head_dim, (uint32_t)p.slots};
 }
 
-// Row blocks with several ranges, times kv heads: half the slots at most, and no
-// more than there are.
-unsigned split_blocks(const PagedCache& c, const Part& p) {
-  return (unsigned)(std::min(p.slots / 2, p.blocks / c.kv_heads) * c.kv_heads);
+// The sum over ranges: blocks for the row blocks that may have several (half the slots
+// at most, and no more than there are), times kv heads, and how many of a row block's
+// rows each takes, so that there are about 2048 in all (each looks its unit up, which
+// costs more than some rows one after the other).
+struct Split {
+  unsigned blocks = 0, parts = 0;
+  int rows = 1;
+};
+
+Split split_of(const PagedCache& c, const Part& p) {
+  Split s;
+  s.blocks = (unsigned)(std::min(p.slots / 2, p.row_blocks) * c.kv_heads);
+  if (!s.blocks) return s;
+  s.parts = std::max(1u, std::min((unsigned)p.most_rows, 2048u / s.blocks));
+  s.rows = (p.most_rows + s.parts - 1) / s.parts;
+  return s;
 }
 
 template <int D, int G>
@@ -750,14 +769,12 @@ hipError_t launch_kv4_attention(const PagedCache& c, const PagedBatch& b, const 
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  const unsigned few_blocks = s.any_few ? split_blocks(c, s.few) : 0;
-  const unsigned many_blocks = s.any_many ? split_blocks(c, s.many) : 0;
-  if (few_blocks + many_blocks == 0) return e;
-  auto parts = [](const Part& p, int rows) { return (p.most_rows + rows - 1) / rows; };
-  const int y = std::max(few_blocks ? parts(s.few, kCombineRows) : 0,
-                         many_blocks ? parts(s.many, kCombineManyRows) : 0);
-  hipLaunchKernelGGL(kv4_attention_combine_kernel, dim3(few_blocks + many_blocks, y), dim3(256), 0,
-                     stream, c, b, a, s.few.u, few, s.many.u, many, (int)few_blocks);
+  const Split fs = s.any_few ? split_of(c, s.few) : Split(),
+              ms = s.any_many ? split_of(c, s.many) : Split();
+  if (fs.blocks + ms.blocks == 0) return e;
+  hipLaunchKernelGGL(kv4_attention_combine_kernel,
+                     dim3(fs.blocks + ms.blocks, std::max(fs.parts, ms.parts)), dim3(256), 0, stream,
+                     c, b, a, s.few.u, few, s.many.u, many, (int)fs.blocks, fs.rows, ms.rows);
   return hipGetLastError();
 }
 
