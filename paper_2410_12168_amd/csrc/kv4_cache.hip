@@ -26,6 +26,9 @@ namespace {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;
+// Heads whose loads a lane has in flight: stores may not be passed by loads, since
+// nothing says that they go elsewhere, so the loads of several heads come first.
+constexpr int kAhead = 4;
 
 __device__ inline float low_half(uint32_t w) {
   return __half2float(__ushort_as_half((unsigned short)w));
@@ -95,20 +98,30 @@ __global__ __launch_bounds__(kThreads) void kv4_append_kernel(PagedCache c, Page
   if (p.page < 0) return;  // all lanes of a row alike
   const int group = c.G / 8;
   const int last = min(2 * c.kv_heads, ((int)blockIdx.y + 1) * per_block);
-  for (int i = blockIdx.y * per_block; i < last; ++i) {
-    const bool v = i >= c.kv_heads;
-    const int head = v ? i - c.kv_heads : i;
-    const uint16_t* x = (v ? r.v_in + m * r.v_stride : r.k_in + m * r.k_stride) +
-                        head * c.head_dim + 8 * chunk;
-    uint32_t codes, param;
-    quantize_group(__builtin_nontemporal_load(reinterpret_cast<const u32x4*>(x)), group, &codes,
-                   &param);
-    const long long row = cache_row(c, p.page, head, p.pos);
-    uint32_t* to = reinterpret_cast<uint32_t*>(v ? c.v_codes : c.k_codes);
-    to[row * lanes + chunk] = codes;
-    if (chunk % group == 0) {
-      uint32_t* params = reinterpret_cast<uint32_t*>(v ? c.v_params : c.k_params);
-      params[(row * c.head_dim + 8 * chunk) / c.G] = param;
+  for (int i0 = blockIdx.y * per_block; i0 < last; i0 += kAhead) {
+    u32x4 x[kAhead];
+    #pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int i = min(i0 + j, last - 1);
+      const bool v = i >= c.kv_heads;
+      const uint16_t* at = (v ? r.v_in + m * r.v_stride : r.k_in + m * r.k_stride) +
+                           (v ? i - c.kv_heads : i) * c.head_dim + 8 * chunk;
+      x[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(at));
+    }
+    #pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int i = i0 + j;
+      if (i >= last) break;
+      const bool v = i >= c.kv_heads;
+      uint32_t codes, param;
+      quantize_group(x[j], group, &codes, &param);
+      const long long row = cache_row(c, p.page, v ? i - c.kv_heads : i, p.pos);
+      uint32_t* to = reinterpret_cast<uint32_t*>(v ? c.v_codes : c.k_codes);
+      to[row * lanes + chunk] = codes;
+      if (chunk % group == 0) {
+        uint32_t* params = reinterpret_cast<uint32_t*>(v ? c.v_params : c.k_params);
+        params[(row * c.head_dim + 8 * chunk) / c.G] = param;
+      }
     }
   }
 }
@@ -122,29 +135,38 @@ __global__ __launch_bounds__(kThreads) void kv4_gather_kernel(PagedCache c, Page
   const Place p = place_of(c, b, m);
   if (!p.in_row) return;
   const int last = min(heads, ((int)blockIdx.y + 1) * per_block);
-  for (int j = blockIdx.y * per_block; j < last; ++j) {
-    const int i = first + j;
-    const bool v = i >= c.kv_heads;
-    const int head = v ? i - c.kv_heads : i;
-    u32x4 o = {0, 0, 0, 0};
-    if (p.page >= 0) {
-      const long long row = cache_row(c, p.page, head, p.pos);
-      const uint32_t q = reinterpret_cast<const uint32_t*>(v ? c.v_codes
-                                                             : c.k_codes)[row * lanes + chunk];
-      const uint32_t param = reinterpret_cast<const uint32_t*>(
-          v ? c.v_params : c.k_params)[(row * c.head_dim + 8 * chunk) / c.G];
-      const float s = low_half(param), mn = low_half(param >> 16);
+  for (int j0 = blockIdx.y * per_block; j0 < last; j0 += kAhead) {
+    uint32_t q[kAhead], param[kAhead];
+    #pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      q[j] = param[j] = 0;
+      if (p.page >= 0) {
+        const int i = first + min(j0 + j, last - 1);
+        const bool v = i >= c.kv_heads;
+        const long long row = cache_row(c, p.page, v ? i - c.kv_heads : i, p.pos);
+        q[j] = reinterpret_cast<const uint32_t*>(v ? c.v_codes : c.k_codes)[row * lanes + chunk];
+        param[j] = reinterpret_cast<const uint32_t*>(
+            v ? c.v_params : c.k_params)[(row * c.head_dim + 8 * chunk) / c.G];
+      }
+    }
+    #pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      if (j0 + j >= last) break;
+      const int i = first + j0 + j;
+      const bool v = i >= c.kv_heads;
+      const float s = low_half(param[j]), mn = low_half(param[j] >> 16);
+      u32x4 o;
       #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const float p0 = (float)((q >> (8 * k)) & 15u) * s;
-        const float p1 = (float)((q >> (8 * k + 4)) & 15u) * s;
+        const float p0 = (float)((q[j] >> (8 * k)) & 15u) * s;
+        const float p1 = (float)((q[j] >> (8 * k + 4)) & 15u) * s;
         o[k] = (uint32_t)__half_as_ushort(__float2half_rn(p0 + mn)) |
                (uint32_t)__half_as_ushort(__float2half_rn(p1 + mn)) << 16;
       }
+      uint16_t* x = (v ? r.v_out + m * r.v_stride : r.k_out + m * r.k_stride) +
+                    (v ? i - c.kv_heads : i) * c.head_dim + 8 * chunk;
+      __builtin_nontemporal_store(o, reinterpret_cast<u32x4*>(x));
     }
-    uint16_t* x = (v ? r.v_out + m * r.v_stride : r.k_out + m * r.k_stride) + head * c.head_dim +
-                  8 * chunk;
-    __builtin_nontemporal_store(o, reinterpret_cast<u32x4*>(x));
   }
 }
 

@@ -15,6 +15,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "../../include/comet.h"
@@ -27,6 +28,9 @@ namespace {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;
+// Heads whose loads a lane has in flight: in place, no load may pass a store, so the
+// loads of several heads come first.
+constexpr int kAhead = 3;
 constexpr double kInvTwoPi = 0.15915494309189533577;
 
 __device__ inline void turn(int position, double freq, float mscale, float* c, float* s) {
@@ -79,40 +83,43 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, int chunks, 
   }
   const uint16_t* x = a.X + m * a.x_stride;
   uint16_t* o = a.out + m * a.out_stride;
-  for (int h = h0; h < h1; h += head_lanes) {
-    const u32x4* xa = reinterpret_cast<const u32x4*>(x + h * a.head_dim + ca);
-    const u32x4* xb = reinterpret_cast<const u32x4*>(x + h * a.head_dim + cb);
-    u32x4* oa = reinterpret_cast<u32x4*>(o + h * a.head_dim + ca);
-    u32x4* ob = reinterpret_cast<u32x4*>(o + h * a.head_dim + cb);
-    if (tail) {
-      *oa = *xa;
-      if (second) *ob = *xb;
-      continue;
+  for (int h = h0; h < h1; h += kAhead * head_lanes) {
+    u32x4 va[kAhead], vb[kAhead];
+    #pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int hj = h + j * head_lanes;
+      if (hj >= h1) break;
+      va[j] = *reinterpret_cast<const u32x4*>(x + hj * a.head_dim + ca);
+      if (second) vb[j] = *reinterpret_cast<const u32x4*>(x + hj * a.head_dim + cb);
     }
-    const u32x4 va = *xa, vb = *xb;
-    u32x4 ra, rb;
-    if (INTERLEAVED) {  // dword = one pair
-      #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        uint32_t lo, hi;
-        rotate(half_bits(va[i]), half_bits(va[i] >> 16), c[i], s[i], &lo, &hi);
-        ra[i] = lo | hi << 16;
-        rotate(half_bits(vb[i]), half_bits(vb[i] >> 16), c[4 + i], s[4 + i], &lo, &hi);
-        rb[i] = lo | hi << 16;
+    #pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int hj = h + j * head_lanes;
+      if (hj >= h1) break;
+      u32x4 ra = va[j], rb = vb[j];
+      if (!tail) {
+        #pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          uint32_t lo, hi;
+          if (INTERLEAVED) {  // dword = one pair
+            rotate(half_bits(va[j][i]), half_bits(va[j][i] >> 16), c[i], s[i], &lo, &hi);
+            ra[i] = lo | hi << 16;
+            rotate(half_bits(vb[j][i]), half_bits(vb[j][i] >> 16), c[4 + i], s[4 + i], &lo, &hi);
+            rb[i] = lo | hi << 16;
+          } else {
+            rotate(half_bits(va[j][i]), half_bits(vb[j][i]), c[2 * i], s[2 * i], &lo, &hi);
+            ra[i] = lo;
+            rb[i] = hi;
+            rotate(half_bits(va[j][i] >> 16), half_bits(vb[j][i] >> 16), c[2 * i + 1],
+                   s[2 * i + 1], &lo, &hi);
+            ra[i] |= lo << 16;
+            rb[i] |= hi << 16;
+          }
+        }
       }
-    } else {
-      #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        uint32_t a0, b0, a1, b1;
-        rotate(half_bits(va[i]), half_bits(vb[i]), c[2 * i], s[2 * i], &a0, &b0);
-        rotate(half_bits(va[i] >> 16), half_bits(vb[i] >> 16), c[2 * i + 1], s[2 * i + 1], &a1,
-               &b1);
-        ra[i] = a0 | a1 << 16;
-        rb[i] = b0 | b1 << 16;
-      }
+      *reinterpret_cast<u32x4*>(o + hj * a.head_dim + ca) = ra;
+      if (second) *reinterpret_cast<u32x4*>(o + hj * a.head_dim + cb) = rb;
     }
-    *oa = ra;
-    *ob = rb;
   }
 }
 
