@@ -170,10 +170,11 @@ __global__ __launch_bounds__(kThreads) void kv4_gather_kernel(PagedCache c, Page
   }
 }
 
-// Heads (of K and V together) per block: all of them once the row blocks alone
-// are two for each compute unit, else fewer, down to one.
+// Heads (of K and V together) per block: as many as leave 8 blocks to a compute unit,
+// whole runs of kAhead where they can be.
 int heads_per_block(int heads, int row_blocks, int cus) {
-  return std::max(1, std::min(heads, heads * row_blocks / (2 * cus)));
+  const int per = std::max(1, std::min(heads, (int)((long long)heads * row_blocks / (8 * cus))));
+  return per > kAhead ? per / kAhead * kAhead : per;
 }
 
 }  // namespace

@@ -89,8 +89,8 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, int chunks, 
     for (int j = 0; j < kAhead; ++j) {
       const int hj = h + j * head_lanes;
       if (hj >= h1) break;
-      va[j] = *reinterpret_cast<const u32x4*>(x + hj * a.head_dim + ca);
-      if (second) vb[j] = *reinterpret_cast<const u32x4*>(x + hj * a.head_dim + cb);
+      va[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(x + hj * a.head_dim + ca));
+      if (second) vb[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(x + hj * a.head_dim + cb));
     }
     #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
@@ -166,11 +166,14 @@ hipError_t launch_rope(const RopeArgs& a, hipStream_t stream) {
   }
   const bool copy = a.X != a.out;
   const int chunks = a.rot_dim / 16 + (copy ? (a.head_dim - a.rot_dim + 15) / 16 : 0);
-  // 8 heads at a time; few rows: a block for each 8 heads as well
+  // 8 heads at a time, and as many in all as leave 8 blocks to a compute unit (an
+  // angle is worked out once per block)
   const int head_lanes = std::max(1, std::min(std::min(8, a.heads), kThreads / chunks));
   const int rows = std::max(1, kThreads / (chunks * head_lanes));
-  const bool few = (a.M + rows - 1) / rows < 2 * a.cus;
-  const int heads_per_block = few ? head_lanes : a.heads;
+  const int blocks = (a.M + rows - 1) / rows, turns = (a.heads + head_lanes - 1) / head_lanes;
+  int per = std::max(1, std::min(turns, (int)((long long)turns * blocks / (8 * a.cus))));
+  if (per > kAhead) per = per / kAhead * kAhead;
+  const int heads_per_block = per * head_lanes;
   const dim3 grid((a.M + rows - 1) / rows, (a.heads + heads_per_block - 1) / heads_per_block);
   if (a.interleaved)
     hipLaunchKernelGGL(rope_kernel<true>, grid, dim3(kThreads), 0, stream, a, chunks, head_lanes,
