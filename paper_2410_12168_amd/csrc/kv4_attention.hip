@@ -660,8 +660,11 @@ Part part_of(const PagedCache& c, const PagedBatch& b, int heads, int window, in
   p.u.low = low;
   p.u.high = high;
   p.most_rows = (int)std::min<long long>(rows, (long long)b.max_rows * p.u.group);
-  // every sequence's last row block may be ragged
-  const long long row_blocks = (long long)b.M * p.u.group / rows + std::min(b.B, b.M);
+  // every sequence's last row block may be ragged; none has more than `high` rows
+  const long long sequences = std::min(b.B, b.M);
+  const long long q_rows = (long long)b.M * p.u.group;
+  const long long row_blocks = std::min(
+      q_rows / rows + sequences, sequences * ((std::min<long long>(high, q_rows) + rows - 1) / rows));
   p.row_blocks = row_blocks;
   const long long tiles = (((long long)b.max_pages << c.page_shift) + kTile - 1) / kTile;
   const long long ranges = (tiles + kMinTiles - 1) / kMinTiles;

@@ -294,6 +294,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
   const int k_at = k_place(col, half);
   const int v_at = V_AT + v_place(4 * half + (lane16 >> 2),
                                   2 * (lane >> 4 & 1) + (lane16 >> 1 & 1)) + 8 * (lane16 & 1);
+  constexpr int AHEAD = NG == 1 ? 8 : 4;  // operands of K that are read ahead
+  f16x8 k[AHEAD], mn;
+  auto k_operand = [&](int buf, int n) {  // of the n-th step, over both halves of the tile
+    return *reinterpret_cast<const f16x8*>(lds + (buf + k_at ^ 32 * (n % KS)) + n / KS * 32 * F);
+  };
+  auto mn_operand = [&](int buf, int t) {
+    return *reinterpret_cast<const f16x8*>(lds + buf + M_AT + 32 * (32 * t + col) + 16 * half);
+  };
   auto work = [&](int buf, int tile, unsigned long long have, unsigned long long poison) {
     const int t0 = tile * kTile;
     const float* params = reinterpret_cast<const float*>(lds + buf + P_AT);
@@ -301,18 +309,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
     // The order below is the intended one: next to each product stand the reads of a
     // later one and other arithmetic, which run while the matrix core works (the
     // next tile's codes, the first half's scores).
-    constexpr int AHEAD = NG == 1 ? 8 : 4;  // operands of K that are read ahead
     f32x16 x[2];
-    f16x8 k[AHEAD], mn;
-    auto k_operand = [&](int n) {  // of the n-th step, over both halves of the tile
-      return *reinterpret_cast<const f16x8*>(lds + (buf + k_at ^ 32 * (n % KS)) + n / KS * 32 * F);
-    };
-    auto mn_operand = [&](int t) {
-      return *reinterpret_cast<const f16x8*>(lds + buf + M_AT + 32 * (32 * t + col) + 16 * half);
-    };
-    mn = mn_operand(0);
-    #pragma unroll
-    for (int n = 0; n < AHEAD; ++n) k[n] = k_operand(n);
     f32x16 zero;
     #pragma unroll
     for (int i = 0; i < 16; ++i) zero[i] = 0.0f;
@@ -320,7 +317,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
     for (int t = 0; t < 2; ++t) {
       __builtin_amdgcn_sched_barrier(0);
       x[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(mn, qsums, zero, 0, 0, 0);
-      if (t == 0) mn = mn_operand(1);
+      if (t == 0) mn = mn_operand(buf, 1);
       #pragma unroll
       for (int g = 0; g < NG; ++g) {
         f32x16 d = zero;
@@ -328,7 +325,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
         for (int s = g * KS / NG; s < (g + 1) * KS / NG; ++s) {
           const int n = t * KS + s;
           d = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[n % AHEAD], q[s], d, 0, 0, 0);
-          if (n + AHEAD < 2 * KS) k[n % AHEAD] = k_operand(n + AHEAD);
+          if (n + AHEAD < 2 * KS) k[n % AHEAD] = k_operand(buf, n + AHEAD);
           if (n % 2 == 0) {
             #pragma unroll
             for (int i = n / 2 * 2 * KD / KS; i < (n / 2 + 1) * 2 * KD / KS; ++i)
@@ -464,6 +461,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
       // registers of q
       asm volatile("" : "+s"(buf));
       __syncthreads();  // the tile is in LDS, and the other buffer is free
+      mn = mn_operand(buf, 0);
+      #pragma unroll
+      for (int n = 0; n < AHEAD; ++n) k[n] = k_operand(buf, n);
       // the next tile is staged on the way (after the last one, once more to no end)
       if (tile + 1 < tile1) stage_params(BUF - buf);
       const unsigned long long have_next = held;
