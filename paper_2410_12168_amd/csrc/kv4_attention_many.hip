@@ -86,9 +86,65 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
   const int seq_row = (row0 + wave_row + col) / u.group;
   const int q_head = head * u.group + (row0 + wave_row + col) % u.group;
   const int pos = w.len - w.n + seq_row;
+  // ---- pages: lane 4 i + k has the slab (page and head) of granule k (16 tokens) of
+  // the i-th next tile, or -1
+  const int32_t* table = b.block_table + (long long)unit.seq * b.max_pages;
+  const bool one_page = c.page_shift >= 6;  // a tile lies in one
+  int slabs = -1;
+  auto load_pages = [&](int tile) {
+    const int i = (tile * kTile + 16 * lane) >> c.page_shift;
+    slabs = slab_of(c, head, i < b.max_pages ? table[i] : -1);
+  };
+  // ---- loads of a tile: a thread takes a quarter of the codes of one token of its
+  // wave's granule, and the parameters of token `lane`
+  const int token = 16 * wave + (lane & 15), quarter = lane >> 4;
+  uint32_t kreg[KD], vreg[KD], preg[2][NG];
+  unsigned long long held = 0;  // tokens that are in the cache
+  auto load = [&](int tile, int ahead) {
+    const int t = tile * kTile;
+    int slab[4];
+    slab[0] = __builtin_amdgcn_readlane(slabs, 4 * ahead);
+    long long row = slab_row(c, slab[0], t), mine = row + (lane & 48);
+    row += 16 * wave;
+    held = slab[0] >= 0 ? ~0ull : 0;
+    if (!one_page) {
+      #pragma unroll
+      for (int k = 1; k < 4; ++k) slab[k] = __builtin_amdgcn_readlane(slabs, 4 * ahead + k);
+      row = slab_row(c, wave < 2 ? (wave ? slab[1] : slab[0]) : (wave == 2 ? slab[2] : slab[3]),
+                     t + 16 * wave);
+      mine = slab_row(c, quarter < 2 ? (quarter ? slab[1] : slab[0])
+                                     : (quarter == 2 ? slab[2] : slab[3]), t + 16 * quarter);
+      held = 0;
+      #pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (slab[k] >= 0) held |= 0xFFFFull << (16 * k);
+    }
+    const int left = w.len - t;
+    if (left < kTile) held &= (1ull << max(left, 0)) - 1;
+    const unsigned at = (lane & 15) * ROW + ROW / 4 * quarter;
+    if constexpr (KD == 4) {
+      const u32x4 k = *reinterpret_cast<const u32x4*>(c.k_codes + row * ROW + at);
+      const u32x4 v = *reinterpret_cast<const u32x4*>(c.v_codes + row * ROW + at);
+      #pragma unroll
+      for (int i = 0; i < 4; ++i) kreg[i] = k[i], vreg[i] = v[i];
+    } else {
+      const u32x2 k = *reinterpret_cast<const u32x2*>(c.k_codes + row * ROW + at);
+      const u32x2 v = *reinterpret_cast<const u32x2*>(c.v_codes + row * ROW + at);
+      #pragma unroll
+      for (int i = 0; i < 2; ++i) kreg[i] = k[i], vreg[i] = v[i];
+    }
+    const long long p = (mine + (lane & 15)) * NG;
+    #pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      preg[0][g] = reinterpret_cast<const uint32_t*>(c.k_params)[p + g];
+      preg[1][g] = reinterpret_cast<const uint32_t*>(c.v_params)[p + g];
+    }
+  };
+
+  if (tile0 < tile1) load_pages(tile0);
+
   f16x8 q[KS];
   float qsum[NG], offset[NG];
-  float big = 0.0f;
   u32x4 raw[KS];
   #pragma unroll
   for (int s = 0; s < KS; ++s) {
@@ -96,10 +152,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
     if (live)
       raw[s] = *reinterpret_cast<const u32x4*>(a.Q + (long long)(w.start + seq_row) * a.q_stride +
                                                q_head * D + 16 * s + 8 * half);
+  }
+  if (tile0 < tile1) load(tile0, 0);  // in flight while q is converted
+  float big = 0.0f;
+  #pragma unroll
+  for (int s = 0; s < KS; ++s)
     #pragma unroll
     for (int k = 0; k < 4; ++k)
       big = fmaxf(big, fmaxf(fabsf(low_half(raw[s][k])), fabsf(low_half(raw[s][k] >> 16))));
-  }
   big = pair_max(big);
   int e = 10;
   if (big > 0.0f && big < INFINITY) e = ilogbf(big);
@@ -156,61 +216,6 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
     #pragma unroll
     for (int k = 0; k < 16; ++k) o[d][k] = 0.0f;
   int vexp = -24;  // the exponent below that `o` goes by
-
-  // ---- pages: lane 4 i + k has the slab (page and head) of granule k (16 tokens) of
-  // the i-th next tile, or -1
-  const int32_t* table = b.block_table + (long long)unit.seq * b.max_pages;
-  const bool one_page = c.page_shift >= 6;  // a tile lies in one
-  int slabs = -1;
-  auto load_pages = [&](int tile) {
-    const int i = (tile * kTile + 16 * lane) >> c.page_shift;
-    slabs = slab_of(c, head, i < b.max_pages ? table[i] : -1);
-  };
-  // ---- loads of a tile: a thread takes a quarter of the codes of one token of its
-  // wave's granule, and the parameters of token `lane`
-  const int token = 16 * wave + (lane & 15), quarter = lane >> 4;
-  uint32_t kreg[KD], vreg[KD], preg[2][NG];
-  unsigned long long held = 0;  // tokens that are in the cache
-  auto load = [&](int tile, int ahead) {
-    const int t = tile * kTile;
-    int slab[4];
-    slab[0] = __builtin_amdgcn_readlane(slabs, 4 * ahead);
-    long long row = slab_row(c, slab[0], t), mine = row + (lane & 48);
-    row += 16 * wave;
-    held = slab[0] >= 0 ? ~0ull : 0;
-    if (!one_page) {
-      #pragma unroll
-      for (int k = 1; k < 4; ++k) slab[k] = __builtin_amdgcn_readlane(slabs, 4 * ahead + k);
-      row = slab_row(c, wave < 2 ? (wave ? slab[1] : slab[0]) : (wave == 2 ? slab[2] : slab[3]),
-                     t + 16 * wave);
-      mine = slab_row(c, quarter < 2 ? (quarter ? slab[1] : slab[0])
-                                     : (quarter == 2 ? slab[2] : slab[3]), t + 16 * quarter);
-      held = 0;
-      #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (slab[k] >= 0) held |= 0xFFFFull << (16 * k);
-    }
-    const int left = w.len - t;
-    if (left < kTile) held &= (1ull << max(left, 0)) - 1;
-    const unsigned at = (lane & 15) * ROW + ROW / 4 * quarter;
-    if constexpr (KD == 4) {
-      const u32x4 k = *reinterpret_cast<const u32x4*>(c.k_codes + row * ROW + at);
-      const u32x4 v = *reinterpret_cast<const u32x4*>(c.v_codes + row * ROW + at);
-      #pragma unroll
-      for (int i = 0; i < 4; ++i) kreg[i] = k[i], vreg[i] = v[i];
-    } else {
-      const u32x2 k = *reinterpret_cast<const u32x2*>(c.k_codes + row * ROW + at);
-      const u32x2 v = *reinterpret_cast<const u32x2*>(c.v_codes + row * ROW + at);
-      #pragma unroll
-      for (int i = 0; i < 2; ++i) kreg[i] = k[i], vreg[i] = v[i];
-    }
-    const long long p = (mine + (lane & 15)) * NG;
-    #pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      preg[0][g] = reinterpret_cast<const uint32_t*>(c.k_params)[p + g];
-      preg[1][g] = reinterpret_cast<const uint32_t*>(c.v_params)[p + g];
-    }
-  };
 
   // Where a 16-byte chunk (8 channels) of a token lies in LDS.
   auto k_place = [](int t, int chunk) {
@@ -446,8 +451,6 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
   };
 
   if (tile0 < tile1) {
-    load_pages(tile0);
-    load(tile0, 0);
     stage_params(0);
     #pragma unroll
     for (int i = 0; i < 2 * KD; ++i) stage_codes(0, i);
