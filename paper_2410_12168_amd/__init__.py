@@ -606,18 +606,18 @@ def rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "none",
 
 # torch and its lookup of the current device, once a wrapper below has needed
 # them.  These wrappers run several times per layer and token, so an argument that
-# is as it should be passes with few lookups.  (rope of one token: 6.5 us a call
+# is as it should be passes with few lookups.  (rope of one token: 6.7 us a call
 # when each check was made by itself, of which the library's own part is 3.3.)
 _torch = None
 _current_device = None
-_float16 = None
+_float16 = _float64 = _int32 = None
 
 
 def _need_torch():
-    global _torch, _current_device, _float16
+    global _torch, _current_device, _float16, _float64, _int32
     import torch
 
-    _float16 = torch.float16
+    _float16, _float64, _int32 = torch.float16, torch.float64, torch.int32
     if not torch.cuda.is_available():
         _current_device = lambda: -2  # where no tensor is
     else:
@@ -671,10 +671,9 @@ def _explain(t, name: str, here: int) -> None:
 
 
 def _plain(t, dtype: str, name: str, here: int) -> None:
-    """_tensor, on device `here`."""
+    """Raises unless t is what _tensor asks for, on device `here`."""
     _tensor(t, dtype, name)
-    if t.get_device() != here:
-        _explain(t, name, here)
+    _explain(t, name, here)
 
 
 def _new(shape, dtype, device, stream):
@@ -696,9 +695,12 @@ def rope(x, positions, freqs, interleaved: bool = False, mscale: float = 1.0, ou
     ``rope_frequencies``, on the GPU.  Returns out (out=x rotates in place)."""
     here = _here()
     M, H, D, xs = _heads_of(x, "x", here)
-    _plain(positions, "int32", "positions", here)
-    _plain(freqs, "float64", "freqs", here)
-    _exact(positions, M, "positions")
+    for t, dtype, name in ((positions, _int32, "positions"), (freqs, _float64, "freqs")):
+        if not (type(t) is _torch.Tensor and t.dtype is dtype and t.get_device() == here
+                and t.is_contiguous()):
+            _plain(t, str(dtype)[6:], name, here)
+    if positions.numel() != M:
+        _exact(positions, M, "positions")
     if out is None:
         out = _new((M, H, D), _torch.float16, x.device, stream)
         os_ = H * D
@@ -706,9 +708,11 @@ def rope(x, positions, freqs, interleaved: bool = False, mscale: float = 1.0, ou
         oM, oH, oD, os_ = _heads_of(out, "out", here)
         if oM != M or oH != H or oD != D:
             raise ValueError(f"out: shape {tuple(out.shape)}, expected {(M, H, D)}")
-    _check(lib().comet_rope(x.data_ptr(), positions.data_ptr(), freqs.data_ptr(), out.data_ptr(),
-                            M, H, D, 2 * freqs.numel(), xs, os_, 1 if interleaved else 0, mscale,
-                            _stream(stream)))
+    status = (_lib or lib()).comet_rope(x.data_ptr(), positions.data_ptr(), freqs.data_ptr(),
+                                        out.data_ptr(), M, H, D, 2 * freqs.numel(), xs, os_,
+                                        1 if interleaved else 0, mscale, _stream(stream))
+    if status:
+        _check(status)
     return out
 
 
@@ -810,8 +814,10 @@ def kv4_append(cache: KV4Cache, batch: KV4Batch, k, v, stream=None) -> None:
     buffer) into the cache, each to its sequence's last positions."""
     here = _kv4_here(cache, batch)
     ks, vs = _kv4_rows(k, cache, batch, "k", here), _kv4_rows(v, cache, batch, "v", here)
-    _check(lib().comet_kv4_append(cache.address, batch.address, k.data_ptr(), v.data_ptr(), ks, vs,
-                                  _stream(stream)))
+    status = (_lib or lib()).comet_kv4_append(cache.address, batch.address, k.data_ptr(),
+                                              v.data_ptr(), ks, vs, _stream(stream))
+    if status:
+        _check(status)
 
 
 def kv4_gather(cache: KV4Cache, batch: KV4Batch, k_out=None, v_out=None, stream=None):
@@ -825,8 +831,10 @@ def kv4_gather(cache: KV4Cache, batch: KV4Batch, k_out=None, v_out=None, stream=
         v_out = _new(shape, _torch.float16, cache.device, stream)
     ks = _kv4_rows(k_out, cache, batch, "k_out", here)
     vs = _kv4_rows(v_out, cache, batch, "v_out", here)
-    _check(lib().comet_kv4_gather(cache.address, batch.address, k_out.data_ptr(), v_out.data_ptr(),
-                                  ks, vs, _stream(stream)))
+    status = (_lib or lib()).comet_kv4_gather(cache.address, batch.address, k_out.data_ptr(),
+                                              v_out.data_ptr(), ks, vs, _stream(stream))
+    if status:
+        _check(status)
     return k_out, v_out
 
 
@@ -874,10 +882,12 @@ def kv4_attention(q, cache: KV4Cache, batch: KV4Batch, scale: Optional[float] = 
         workspace = kv4_attention_workspace(q, cache, batch, stream)
     else:
         _plain(workspace, "uint8", "workspace", here)
-    _check(lib().comet_kv4_attention(
+    status = (_lib or lib()).comet_kv4_attention(
         cache.address, batch.address, q.data_ptr(), out.data_ptr(), H, qs, os_,
         D ** -0.5 if scale is None else scale, window, workspace.data_ptr(), workspace.numel(),
-        _stream(stream)))
+        _stream(stream))
+    if status:
+        _check(status)
     return out
 
 
