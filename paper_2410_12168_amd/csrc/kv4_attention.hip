@@ -566,7 +566,9 @@ __global__ __launch_bounds__(256) void kv4_attention_combine_kernel(PagedCache c
   const int group = threadIdx.x / lanes, channel = 4 * (threadIdx.x % lanes);
   const int turn = group % turns, at_once = groups / turns;
   const int row0 = unit.block * u.rows + blockIdx.y * my_rows;
-  const int rows = min(my_rows, unit.w.n * u.group - row0);
+  // not those of the next row block, nor behind the sequence's last
+  const int rows = min(min(my_rows, u.rows - (int)blockIdx.y * my_rows),
+                       unit.w.n * u.group - row0);
   for (int r0 = 0; r0 < rows; r0 += at_once) {
     const int r = r0 + group / turns, row = row0 + r;
     const bool live = r < rows;

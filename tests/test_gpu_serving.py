@@ -265,6 +265,8 @@ ATTENTION = [
     ([(150, 300)], 8, 2, 128, 128, 16, 33),
     ([(150, 150), (90, 700)], 4, 2, 128, 128, 64, 200),
     ([(100, 120)], 4, 4, 64, 32, 16, 5000),
+    ([(130, 1500)], 32, 8, 64, 64, 16, 0),  # ranges added up in threes of 128 rows
+    ([(1, 900), (1, 1300), (0, 0), (1, 70), (90, 1600)], 32, 8, 64, 64, 32, 0),
 ]
 
 
