@@ -86,6 +86,13 @@ __device__ inline f16x8 codes_f16(uint32_t x) {
   return __builtin_bit_cast(f16x8, r);
 }
 
+// The same of codes less 8, exact as well: for V, whose weights are rounded.  An
+// error of a weight counts times the code, so codes around 0 take most of it away.
+__device__ inline f16x8 centered_f16(uint32_t x) {
+  const u32x4 eight = {0x80088008u, 0x80808080u, 0x80088008u, 0x80808080u};  // -8 of each
+  return codes_f16(x) + __builtin_bit_cast(f16x8, eight);
+}
+
 // Whether a {scale, offset} pair of fp16 numbers holds an infinity or not-a-number.
 __device__ inline bool not_finite(uint32_t p) {
   return (p & 0x7C00u) == 0x7C00u || (p & 0x7C000000u) == 0x7C000000u;

@@ -161,7 +161,7 @@ __global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_few
 
   // ---- q: operand [step] of each column block, its sums and factor
   f16x8 q[C][KS];
-  float qsum[C][NG], kappa[C], top[C], weight_sum[C], offset[C][NG];
+  float qsum[C][NG], kappa[C], top[C], weight_sum[C], offset[C][NG], rounded[C][NG];
   int pos[C];
   u32x4 raw_q[C][KS];
   #pragma unroll
@@ -225,7 +225,7 @@ __global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_few
     top[cb] = kNone;
     weight_sum[cb] = 0.0f;
     #pragma unroll
-    for (int g = 0; g < NG; ++g) offset[cb][g] = 0.0f;
+    for (int g = 0; g < NG; ++g) offset[cb][g] = rounded[cb][g] = 0.0f;
   }
 
   f32x4 o[C][DB];
@@ -321,7 +321,10 @@ __global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_few
         top[cb] = next[cb];
         weight_sum[cb] *= f;
         #pragma unroll
-        for (int g = 0; g < NG; ++g) offset[cb][g] *= f;
+        for (int g = 0; g < NG; ++g) {
+          offset[cb][g] *= f;
+          rounded[cb][g] *= f;
+        }
         #pragma unroll
         for (int d = 0; d < DB; ++d) o[cb][d] *= f;
       }
@@ -357,6 +360,21 @@ __global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_few
           }
         #pragma unroll
         for (int cb = 0; cb < C; ++cb) asm volatile("" : "+v"(offset[cb][g]));
+      }
+      // An error of a rounded weight counts times the code.  8 of each weight as rounded
+      // are taken off and 8 as they were put back (offsets are those of code 8), which
+      // leaves it times the code less 8.
+      #pragma unroll
+      for (int cb = 0; cb < C; ++cb) {
+        #pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const f16x8 v = p[cb][k / 4];
+          const f16x2 pair = {v[2 * (k % 4)], v[2 * (k % 4) + 1]};
+          const _Float16 one = k & 1 ? 16 : 1;  // an odd token's weight is a 16th
+          rounded[cb][g] =
+              __builtin_amdgcn_fdot2(pair, f16x2{one, one}, rounded[cb][g], false);
+        }
+        asm volatile("" : "+v"(rounded[cb][g]));
       }
       #pragma unroll
       for (int d = g * DB / NG; d < (g + 1) * DB / NG; ++d) {
@@ -414,9 +432,12 @@ __global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_few
       // an odd token's weight takes back the 16 of its code
       weight_unit = ldexpf(1.0f, (lane & 1 ? 10 : 14) - e);
       #pragma unroll
-      for (int cb = 0; cb < C; ++cb)
+      for (int cb = 0; cb < C; ++cb) {
+        #pragma unroll
+        for (int g = 0; g < NG; ++g) rounded[cb][g] *= f;
         #pragma unroll
         for (int d = 0; d < DB; ++d) o[cb][d] *= f;
+      }
     }
     #pragma unroll
     for (int g = 0; g < NG; ++g) {
@@ -424,7 +445,7 @@ __global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_few
       at[0] = low_half(preg[0][g]);
       at[kTile] = low_half(preg[0][g] >> 16);
       at[2 * kTile] = low_half(preg[1][g]) * weight_unit;
-      at[3 * kTile] = low_half(preg[1][g] >> 16);
+      at[3 * kTile] = fmaf(8.0f, low_half(preg[1][g]), low_half(preg[1][g] >> 16));  // of code 8
     }
     #pragma unroll
     for (int i = 0; i < VL; ++i) {
@@ -463,7 +484,7 @@ __global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_few
     }
     #pragma unroll
     for (int g = 0; g < NG; ++g) {
-      const float v = quad_sum(offset[cb][g]);
+      const float v = quad_sum(fmaf(rounded[cb][g], ldexpf(-8.0f, vexp - 14), offset[cb][g]));
       if (quad == 0) at[2 + g] = v;
     }
   }

@@ -237,7 +237,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
   auto stage_codes = [&](int buf, int piece) {
     const int to = piece & 1 ? v_to : k_to, i = piece / 2;
     *reinterpret_cast<f16x8*>(lds + (buf + to ^ 16 * i)) =
-        codes_f16(piece & 1 ? vreg[i] : kreg[i]);
+        piece & 1 ? centered_f16(vreg[i]) : codes_f16(kreg[i]);
   };
   auto stage_params = [&](int buf) {
     const bool stored = held >> lane & 1;
@@ -277,7 +277,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
     for (int g = 0; g < NG; ++g) {
       if (wave == 0) at[3 * g * kTile] = low_half(preg[0][g]) * 65536.0f;
       if (wave == 1) at[(3 * g + 1) * kTile] = low_half(preg[1][g]) * weight_unit;
-      if (wave == 2) at[(3 * g + 2) * kTile] = low_half(preg[1][g] >> 16);
+      if (wave == 2)  // of code 8, V's zero
+        at[(3 * g + 2) * kTile] = fmaf(8.0f, low_half(preg[1][g]), low_half(preg[1][g] >> 16));
     }
     if (wave == 3) {
       uint32_t* m = reinterpret_cast<uint32_t*>(lds + buf + M_AT + 32 * lane);
