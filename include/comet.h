@@ -294,7 +294,7 @@ typedef struct {
  *   row_start    device int32 [B + 1], ascending: rows row_start[b] ..
  *                row_start[b + 1] - 1 are sequence b's (none: an idle
  *                sequence).  Rows in no sequence are neither read nor written.
- *   seq_lens     device int32 [B]: L_b, tokens of sequence b, the rows of this
+ *   seq_lens     device int32 [B]: L_b <= 2^30, tokens of sequence b, the rows of this
  *                call included: row i of n_b is at position L_b - n_b + i.
  *                Rows at negative positions have no token.
  *   block_table  device int32 [B][max_pages]: token j of sequence b lies at

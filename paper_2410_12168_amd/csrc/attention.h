@@ -205,7 +205,7 @@ __device__ inline bool find_unit(const PagedBatch& b, int page_shift, const Unit
       out->slot = from_lane(slots_upto - slots, at) + block * out->ranges + out->range;
       // the last row blocks see the most tokens: they come first
       out->block = out->w.blocks - 1 - block;
-      return true;
+      return block < out->w.blocks;  // (the sums may have run over)
     }
     before = from_lane(upto, 63);
     slots_before = from_lane(slots_upto, 63);

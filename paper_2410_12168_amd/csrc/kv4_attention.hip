@@ -579,7 +579,8 @@ __global__ __launch_bounds__(256) void kv4_attention_combine_kernel(PagedCache c
   if ((int)blockIdx.y * my_rows >= u.rows) return;
   Unit unit;
   if (!find_unit<true>(b, c.page_shift, u, index / c.kv_heads, &unit)) return;
-  if (unit.slot + unit.ranges > part.slots) return;  // no batch that comet.h allows
+  // no batch that comet.h allows
+  if ((unsigned long long)unit.slot + unit.ranges > part.slots) return;
   const int head = index % c.kv_heads;
   const int D = c.head_dim, lanes = D / 4, groups = 256 / lanes;
   int turns = 1;

@@ -284,6 +284,66 @@ def test_attention(seqs, H, kvh, D, G, page, window):
     assert torch.equal(out.view(torch.int16), again.view(torch.int16))
 
 
+@pytest.mark.parametrize("page", [16, 128])
+@pytest.mark.parametrize("n", [1, 20, 100])
+@pytest.mark.parametrize("D,G", [(64, 32), (64, 64), (128, 32), (128, 64), (128, 128)])
+def test_attention_in_every_form(D, G, n, page):
+    # few rows in blocks of 16 and of 32, many rows; tiles within a page and over several;
+    # one range and several
+    p = Paged(D + G + n + page, [(n, 150 + n), (1, 40), (n, 700)], 2, D, G, page)
+    cache, batch = handles(p, max_rows=n)
+    q16 = to16(p.rng.standard_normal((p.M, 4, D)))
+    out = comet.kv4_attention(dev16(q16), cache, batch)
+    ref, bound = p.attention(q16, 4, D ** -0.5)
+    check_attention(host16(out), ref, bound)
+
+
+@pytest.mark.parametrize("window", [0, 50])
+def test_more_sequences_than_lanes_of_a_wave(window):
+    # 150 sequences, some idle, of one row, of some and of many; ranges and whole ones
+    seqs = [((0, 1, 1, 9, 40, 90)[b % 6], 90 + 37 * (b % 30)) for b in range(150)]
+    p = Paged(41, seqs, 1, 64, 64, 32)
+    cache, batch = handles(p, max_rows=90)
+    q16 = to16(p.rng.standard_normal((p.M, 3, 64)))
+    out = comet.kv4_attention(dev16(q16), cache, batch, window=window)
+    ref, bound = p.attention(q16, 3, 0.125, window)
+    check_attention(host16(out), ref, bound)
+
+
+def test_any_device_contents_stay_within_the_buffers():
+    """Row starts that fall, negative lengths and lengths beyond the table, pages out of range:
+    the calls end, and write nothing outside the rows and the cache.  (All indexes are
+    checked where they are made; the buffers have guards on both sides.)"""
+    kvh, H, D, page, M = 2, 8, 64, 16, 40
+    rng = np.random.default_rng(43)
+    shape = (6, kvh, page)
+    whole = [torch.full((10,) + shape[1:] + tail, 7, dtype=t, device=DEV)
+             for tail, t in (((D // 2,), torch.uint8), ((2, 2), torch.float16))]
+    guard = [t.clone() for t in whole]
+    codes, params = whole[0][2:8], whole[1][2:8]
+    rows = [torch.full((M + 4, n, D), 3.0, dtype=torch.float16, device=DEV) for n in (H, kvh)]
+    for k in range(20):
+        B = (1, 3, 70)[k % 3]
+        start = rng.integers(-5, M + 9, B + 1).astype(np.int32)
+        if k % 2:
+            start.sort()
+        lens = rng.integers(-40, 300, B).astype(np.int32)
+        lens[0] = (2 ** 31 - 1, -2 ** 31, 1 << 30, 77)[k % 4]
+        table = rng.integers(-3, 9, (B, 5)).astype(np.int32)
+        batch = comet.KV4Batch(dev(start), dev(lens), dev(table), M)
+        cache = comet.KV4Cache(codes, params, codes, params)
+        q = torch.randn((M, H, D), device=DEV).half()
+        print(f"contents {k}: {start[:4]} {lens[:3]}", flush=True)
+        comet.kv4_append(cache, batch, q[:, :kvh], q[:, kvh:2 * kvh])
+        comet.kv4_gather(cache, batch, k_out=rows[1][2:M + 2], v_out=rows[1][2:M + 2])
+        comet.kv4_attention(q, cache, batch, out=rows[0][2:M + 2], window=(0, 3, 2 ** 31 - 1)[k % 3])
+        torch.cuda.synchronize()
+        for t, g in zip(whole, guard):
+            assert torch.equal(t[:2], g[:2]) and torch.equal(t[8:], g[8:])
+        for t in rows:
+            assert (t[:2] == 3).all() and (t[M + 2:] == 3).all()
+
+
 @pytest.mark.parametrize("n", [1, 40])
 def test_attention_around_holes(n):
     # first, inner and last pages; the whole of one sequence
