@@ -659,9 +659,10 @@ __global__ __launch_bounds__(256) void kv4_attention_combine_kernel(PagedCache c
 
 // ---- host ------------------------------------------------------------------------
 
-// Sequences of up to kFewRows q rows (rows times heads of a group) run on the
-// kernel above, in blocks of 16 or 32; the others on the kernel for many rows.
-constexpr int kFewRows = 64;
+// Sequences of up to this many q rows (rows times heads of a group) run on the kernel
+// above, the others on the kernel for many rows; `narrow`: the launch's q rows are so
+// few that the split along the tokens fills the device.
+int few_rows(bool narrow) { return narrow ? 96 : 64; }
 constexpr int kAny = 0x7FFFFFFF;
 
 // What one of the two kernels does of a batch.
@@ -704,16 +705,17 @@ struct Shape {
 };
 
 Shape shape_of(const PagedCache& c, const PagedBatch& b, int heads, int window, int cus) {
-  const long long most = (long long)b.max_rows * (heads / c.kv_heads);
+  const long long most = (long long)b.max_rows * (heads / c.kv_heads), blocks16 = (most + 15) / 16;
+  const bool narrow = 2 * std::min(b.B, b.M) * blocks16 * c.kv_heads < cus;
   Shape s;
-  s.any_many = most > kFewRows;
+  s.any_many = most > few_rows(narrow);
   // Sequences of few rows among others get a launch of their own, except where most
   // sequences must have about as many rows as the longest
   s.any_few = !s.any_many || 4ll * b.M < 3ll * b.B * b.max_rows;
-  s.columns = most > 16 ? 2 : 1;
+  s.columns = s.any_many || narrow || blocks16 % 2 ? 1 : 2;
   s.few = part_of(c, b, heads, window, cus, 16 * s.columns, s.columns == 1 ? 3 : 2, 0,
-                  s.any_many ? kFewRows : kAny);
-  s.many = part_of(c, b, heads, window, cus, kManyRows, 2, s.any_few ? kFewRows : 0, kAny);
+                  s.any_many ? few_rows(narrow) : kAny);
+  s.many = part_of(c, b, heads, window, cus, kManyRows, 2, s.any_few ? few_rows(narrow) : 0, kAny);
   return s;
 }
 
