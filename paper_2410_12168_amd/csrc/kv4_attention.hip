@@ -29,12 +29,31 @@
 //     the tokens whose scores it has: the weights go from one product into the
 //     other in place.
 //
+// V's codes count around 8: sum p c = sum p (c - 8) + 8 sum p, with the same rounded
+// weights p in both sums, and the exact weights in the offsets' sum of the codes' 8.
+// An error of a weight then counts times |c - 8| instead of c (outputs 3.1e-4 off 64
+// bits in the mean without, 2.2e-4 with; rounding the output alone gives 2.1e-4).
+//
 // Work decomposition: a block of four waves takes one (sequence, kv head, 16 C
 // rows of its q heads, range of tokens); the waves take turns at its 64-token
 // tiles and add up in LDS at the end.  The token ranges follow from the lengths
 // on the device (find_unit): every block of every sequence gets about the same
 // number of tiles, about `target` ranges in all, and a second kernel adds up the
 // ranges of a sequence that has more than one.
+//
+// What bounds it (64 q heads over 8 of 128 channels where nothing else is said; event
+// times of a call, floors at the 4.9 TB/s of a large copy):
+//   - 64 users of up to 8192 tokens (284 MB): 74 us, 3.8 TB/s, floor 57.  The waves
+//     wait for the cache: each has the next tile's codes in flight, three blocks on a
+//     compute unit, and the last blocks end alone.  Two thirds or twice the token
+//     ranges run within 2%.
+//   - one user of 131072 tokens, 32 heads (143 MB): 39 us, 3.6 TB/s, floor 29, of which
+//     the sum over 96 ranges and the launches are 8.  Fewer or more ranges: 37 us
+//     with two thirds, 44 with 4/3.
+//   - one user of 100 tokens: 7 us, latency: two tiles a wave at most, but a table, a
+//     tile and a row of q to fetch one after the other, then the waves' sums.
+//   - 16 users with 5 drafted rows each, 12 heads of 64 channels, up to 2000 tokens:
+//     16 us (floor 3), 12 of it this kernel and 5 the sum over ranges.
 #include <algorithm>
 
 #include "attention.h"
@@ -45,8 +64,13 @@ namespace {
 
 // ---- the products --------------------------------------------------------------
 
+// Blocks that a compute unit holds at a time, as the registers allow.
+__host__ __device__ constexpr int resident_few(int D, int C) {
+  return (C == 1 ? 3 : 2) + (D == 64 ? 1 : 0);
+}
+
 template <int D, int G, int C>
-__global__ __launch_bounds__(64 * kWaves, C == 1 ? 3 : 2) void kv4_attention_few_kernel(
+__global__ __launch_bounds__(64 * kWaves, resident_few(D, C)) void kv4_attention_few_kernel(
     PagedCache c, PagedBatch b, AttentionArgs a, UnitShape u, Partials part) {
   constexpr int NG = D / G;         // groups of a head
   constexpr int KS = D / 32;        // steps of the score product
@@ -564,7 +588,8 @@ constexpr int kAhead = 8;  // ranges that a group has in flight
 
 __global__ __launch_bounds__(256) void kv4_attention_combine_kernel(PagedCache c, PagedBatch b,
                                                                     AttentionArgs a,
-                                                                    UnitShape few, Partials few_part,
+                                                                    UnitShape few,
+                                                                    Partials few_part,
                                                                     UnitShape many,
                                                                     Partials many_part,
                                                                     int few_blocks, int few_rows,
@@ -660,9 +685,14 @@ __global__ __launch_bounds__(256) void kv4_attention_combine_kernel(PagedCache c
 // ---- host ------------------------------------------------------------------------
 
 // Sequences of up to this many q rows (rows times heads of a group) run on the kernel
-// above, the others on the kernel for many rows; `narrow`: the launch's q rows are so
-// few that the split along the tokens fills the device.
-int few_rows(bool narrow) { return narrow ? 96 : 64; }
+// above, the others on the kernel for many rows, whose 128 rows to a block are then
+// used by half at least; `narrow`: the launch's row blocks are fewer than half the
+// compute units, and the split along the tokens fills the device.  Here and there, us:
+//   64 rows of 64 users, 2048 tokens   69   92      96 rows of them   99   96
+//   64 rows of 16 users, 4096 tokens   43   58      96 rows of them   58   63
+//   64 rows of one user, 16384 tokens  21   28      96 rows           24   29
+//   (32-channel groups, 96 rows of 64 users 162 and 148, of one user 34 and 37)
+int most_few(bool narrow) { return narrow ? 96 : 64; }
 constexpr int kAny = 0x7FFFFFFF;
 
 // What one of the two kernels does of a batch.
@@ -674,22 +704,25 @@ struct Part {
   int most_rows;     // of one
 };
 
-// `resident`: blocks that a compute unit holds at a time.
+// Blocks of a compute unit: `aim` to aim at, `resident` at a time.  (64-channel blocks
+// are one more at a time, but shorter, so that their fixed part counts: aiming at one
+// more ran 16 users of 2048 tokens in 17.4 us instead of 15.8.)
 Part part_of(const PagedCache& c, const PagedBatch& b, int heads, int window, int cus, int rows,
-             int resident, int low, int high) {
+             int aim, int resident, int low, int high) {
   Part p;
   p.u.group = heads / c.kv_heads;
   p.u.rows = rows;
   p.u.window = window > 1 << 30 ? 0 : window;  // no position is further
-  p.u.target = std::max(1, cus * resident / c.kv_heads);
+  p.u.target = std::max(1, cus * aim / c.kv_heads);
+  p.u.at_once = std::max(1, cus * resident / c.kv_heads);
   p.u.low = low;
   p.u.high = high;
   p.most_rows = (int)std::min<long long>(rows, (long long)b.max_rows * p.u.group);
   // every sequence's last row block may be ragged; none has more than `high` rows
   const long long sequences = std::min(b.B, b.M);
   const long long q_rows = (long long)b.M * p.u.group;
-  const long long row_blocks = std::min(
-      q_rows / rows + sequences, sequences * ((std::min<long long>(high, q_rows) + rows - 1) / rows));
+  const long long each = (std::min<long long>(high, q_rows) + rows - 1) / rows;
+  const long long row_blocks = std::min(q_rows / rows + sequences, sequences * each);
   p.row_blocks = row_blocks;
   const long long tiles = (((long long)b.max_pages << c.page_shift) + kTile - 1) / kTile;
   const long long ranges = (tiles + kMinTiles - 1) / kMinTiles;
@@ -708,14 +741,24 @@ Shape shape_of(const PagedCache& c, const PagedBatch& b, int heads, int window, 
   const long long most = (long long)b.max_rows * (heads / c.kv_heads), blocks16 = (most + 15) / 16;
   const bool narrow = 2 * std::min(b.B, b.M) * blocks16 * c.kv_heads < cus;
   Shape s;
-  s.any_many = most > few_rows(narrow);
+  s.any_many = most > most_few(narrow);
   // Sequences of few rows among others get a launch of their own, except where most
-  // sequences must have about as many rows as the longest
+  // sequences must have about as many rows as the longest: the launch costs 4 us where
+  // no sequence is for it (8 prompts of 512 rows: 348 and 344 us without), the kernel for
+  // many rows takes 8 us and more for a sequence of one row (4 prompts of 512 rows and
+  // 4 single ones: 191 us, 228 without)
   s.any_few = !s.any_many || 4ll * b.M < 3ll * b.B * b.max_rows;
+  // 32 rows to a block, which read the tokens once for all of them, where that leaves no
+  // block half empty and there are blocks enough (us for 16 and 32 rows to a block: 64
+  // users of 2048 tokens and 64 rows 78 and 69, 48 rows 61 and 69; one user of 16384 and
+  // 32 rows 17.6 and 19.5), and not next to sequences of many rows, where few rows are
+  // mostly one token's (64 users of 8192, 32-channel groups, 8 rows: 167 and 210)
   s.columns = s.any_many || narrow || blocks16 % 2 ? 1 : 2;
-  s.few = part_of(c, b, heads, window, cus, 16 * s.columns, s.columns == 1 ? 3 : 2, 0,
-                  s.any_many ? few_rows(narrow) : kAny);
-  s.many = part_of(c, b, heads, window, cus, kManyRows, 2, s.any_few ? few_rows(narrow) : 0, kAny);
+  s.few = part_of(c, b, heads, window, cus, 16 * s.columns, resident_few(128, s.columns),
+                  resident_few(c.head_dim, s.columns), 0,
+                  s.any_many ? most_few(narrow) : kAny);
+  s.many = part_of(c, b, heads, window, cus, kManyRows, 2, 2,
+                   s.any_few ? most_few(narrow) : 0, kAny);
   return s;
 }
 

@@ -18,6 +18,26 @@
 //     turns them.
 //   - 16-byte chunks of a row in LDS change places with the row's number, so that
 //     the reads and writes of 16 lanes meet all banks.
+//   - V's codes count around 8 (c - 8 is as exact, and the offsets are those of code
+//     8), which takes most of the weights' rounding away.
+//
+// 128 rows to a block: with 256 (eight waves) a chunk of 512 rows ran 2.5% faster, but
+// ragged prompts of 2048 rows 6% slower: larger blocks work on more masked tokens, and
+// there are fewer to fill the device.  Two blocks on a compute unit (71 KB of LDS and
+// 256 registers each): one's staging and softmax run beside the other's products.  The
+// last row blocks of a sequence see most tokens and come first, so that short ones
+// fill the end.
+//
+// Bound by the issue of vector operations: per wave and tile of 32 rows x 64 tokens 34
+// products, about 400 other vector operations and 32 exponentials share a SIMD's issue
+// with the second block's wave (measured: 4 products 62 ns, 32 multiply-adds 78, both
+// together 94).  Vector operations issue in 63% of the cycles, the matrix core works in
+// 33%.  A chunk of 512 rows over 16384 tokens, 64 heads of 128 channels (270 GFLOP):
+// 350 to 365 us, 740 to 770 TFLOP/s; a large fp16 library product reaches 1307.  Prompts
+// of up to 2048 rows, four of them, 32 heads: 129 us.  Not kept, as 1 to 5% slower: the
+// weights' sum by a product with a row of ones, scaling and conversion of the weights
+// in one operation, the score products of both halves interleaved, s_setprio around the
+// score products, blocks in order of their length over all sequences.
 #include "attention.h"
 
 namespace comet {

