@@ -785,6 +785,11 @@ Split split_of(const PagedCache& c, const Part& p) {
   if (!s.blocks) return s;
   s.parts = std::max(1u, std::min((unsigned)p.most_rows, 2048u / s.blocks));
   s.rows = (p.most_rows + s.parts - 1) / s.parts;
+  const int at_once = 1024 / c.head_dim;  // rows that a block takes, with few ranges
+  if (s.rows > at_once) {
+    s.rows = s.rows / at_once * at_once;
+    s.parts = (p.most_rows + s.rows - 1) / s.rows;
+  }
   return s;
 }
 
