@@ -47,6 +47,8 @@ namespace {
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
+constexpr int kWeightBits = 6, kScaleBits = 8;
+
 // Maximum and sum over the two lanes of a column (l, l ^ 32).
 __device__ inline float pair_max(float v) {
   uint32_t a = __float_as_uint(v), b = a;
@@ -68,7 +70,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
   constexpr int ROW = D / 2;  // bytes of a row of codes
   constexpr int KD = D / 32;  // dwords of codes that a thread turns into fp16
   constexpr int F = 2 * D;    // bytes of a row of fp16
-  constexpr int PARAMS = 3 * NG * kTile;  // [NG][K's s, V's s, mn][64]
+  // [NG]: K's s [64], V's {s, mn} as fp16, 4 s and 4 mn in turn
+  constexpr int PARAMS = 2 * NG * kTile;
   // of each of the two buffers: K, V, K's offsets (rows of 16 fp16), parameters
   constexpr int V_AT = kTile * F, M_AT = 2 * kTile * F, P_AT = M_AT + kTile * 32;
   constexpr int BUF = P_AT + 4 * PARAMS;
@@ -164,7 +167,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
   if (tile0 < tile1) load_pages(tile0);
 
   f16x8 q[KS];
-  float qsum[NG], offset[NG];
+  float qsum[NG], offset[NG], eights[NG];
   u32x4 raw[KS];
   #pragma unroll
   for (int s = 0; s < KS; ++s) {
@@ -187,7 +190,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
   // above 0, so that an unseen token's -infinity stays one
   const float kappa = fmaxf(ldexpf(fabsf(a.scale) * kLog2e, 8 + e - 10), 0x1p-120f);
   #pragma unroll
-  for (int g = 0; g < NG; ++g) qsum[g] = offset[g] = 0.0f;
+  for (int g = 0; g < NG; ++g) qsum[g] = offset[g] = eights[g] = 0.0f;
   #pragma unroll
   for (int s = 0; s < KS; ++s) {
     float v[8];
@@ -251,7 +254,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
   const int k_to = k_place(token, KD * quarter), v_to = V_AT + v_place(token, KD * quarter);
   int exponent = -24;
   uint32_t limit = 2;
-  float weight_unit = ldexpf(1.0f, 14 - exponent);
+  float scale_unit = ldexpf(1.0f, kScaleBits - exponent);
   unsigned long long poison_next = 0;
   // codes: 2 KD pieces, K's and V's in turn
   auto stage_codes = [&](int buf, int piece) {
@@ -289,16 +292,19 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
       for (int s = 1; s < 64; s <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, s));
       exponent = __builtin_amdgcn_readfirstlane(ilogbf(low_half(m)));
       limit = exponent >= -15 ? (uint32_t)(exponent + 16) << 10 : 1u << (exponent + 25);
-      weight_unit = ldexpf(1.0f, 14 - exponent);
+      scale_unit = ldexpf(1.0f, kScaleBits - exponent);
     }
     // the waves take turns at the parameters, which all of them have
     float* at = reinterpret_cast<float*>(lds + buf + P_AT) + lane;
+    _Float16* v_at = reinterpret_cast<_Float16*>(lds + buf + P_AT) + 8 * (lane >> 2) + (lane & 3);
     #pragma unroll
     for (int g = 0; g < NG; ++g) {
-      if (wave == 0) at[3 * g * kTile] = low_half(preg[0][g]) * 65536.0f;
-      if (wave == 1) at[(3 * g + 1) * kTile] = low_half(preg[1][g]) * weight_unit;
-      if (wave == 2)  // of code 8, V's zero
-        at[(3 * g + 2) * kTile] = fmaf(8.0f, low_half(preg[1][g]), low_half(preg[1][g] >> 16));
+      if (wave == 0) at[2 * g * kTile] = low_half(preg[0][g]) * 65536.0f;
+      if (wave == 1)
+        v_at[2 * (2 * g + 1) * kTile] = (_Float16)(low_half(preg[1][g]) * scale_unit);
+      if (wave == 2)
+        v_at[2 * (2 * g + 1) * kTile + 4] =
+            __builtin_bit_cast(_Float16, (unsigned short)(preg[1][g] >> 16));
     }
     if (wave == 3) {
       uint32_t* m = reinterpret_cast<uint32_t*>(lds + buf + M_AT + 32 * lane);
@@ -361,7 +367,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
         }
         #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const f32x4 scale = *reinterpret_cast<const f32x4*>(params + 3 * g * kTile + 32 * t +
+          const f32x4 scale = *reinterpret_cast<const f32x4*>(params + 2 * g * kTile + 32 * t +
                                                               8 * i + 4 * half);
           #pragma unroll
           for (int r = 0; r < 4; ++r)
@@ -409,38 +415,48 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
       top = next;
       weight_sum *= f;
       #pragma unroll
-      for (int g = 0; g < NG; ++g) offset[g] *= f;
+      for (int g = 0; g < NG; ++g) {
+        offset[g] *= f;
+        eights[g] *= f;
+      }
       #pragma unroll
       for (int d = 0; d < DT; ++d) o[d] *= f;
     }
     // the weighted sum, 16 tokens at a time; the weights of the next 16 are worked out
     // next to the products of these
+    const float shift = kWeightBits - top;
+    const f16x2 ones = {1, 1};
+    f16x2 wt[2][4];  // of 16 tokens and the next: pairs of the 8 that this half has
     auto weights = [&](int st, int i) {  // of tokens 8 i + 4 half .. + 3 of the 16
       #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int k = 8 * (st & 1) + 4 * i + r;
-        const float wt = __builtin_amdgcn_exp2f(fmaf(x[st / 2][k], kappa, -top));
-        x[st / 2][k] = wt;
-        weight_sum += wt;
+      for (int r = 0; r < 2; ++r) {
+        const int k = 8 * (st & 1) + 4 * i + 2 * r;
+        const f16x2 w =
+            f16x2{(_Float16)__builtin_amdgcn_exp2f(fmaf(x[st / 2][k], kappa, shift)),
+                  (_Float16)__builtin_amdgcn_exp2f(fmaf(x[st / 2][k + 1], kappa, shift))};
+        wt[st & 1][2 * i + r] = w;
+        weight_sum = __builtin_amdgcn_fdot2(w, ones, weight_sum, false);
       }
       asm volatile("" : "+v"(weight_sum));  // here and not after the products
     };
     auto operand = [&](int st, int g) {
-      f16x8 p;
+      u32x4 p;
       #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const float* at = params + (3 * g + 1) * kTile + 16 * st + 8 * i + 4 * half;
-        const f32x4 s = *reinterpret_cast<const f32x4*>(at);
-        const f32x4 m = *reinterpret_cast<const f32x4*>(at + kTile);
+        const float* at = params + (2 * g + 1) * kTile + 16 * st + 8 * i + 4 * half;
+        const u32x4 v = *reinterpret_cast<const u32x4*>(at);
         #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float wt = x[st / 2][8 * (st & 1) + 4 * i + r];
-          offset[g] = fmaf(wt, m[r], offset[g]);
-          p[4 * i + r] = (_Float16)(wt * s[r]);
+        for (int r = 0; r < 2; ++r) {
+          const uint32_t sr = v[r], mr = v[2 + r];
+          const f16x2 s = __builtin_bit_cast(f16x2, sr), m = __builtin_bit_cast(f16x2, mr);
+          const f16x2 w = wt[st & 1][2 * i + r], ws = w * s;
+          offset[g] = __builtin_amdgcn_fdot2(w, m, offset[g], false);
+          eights[g] = __builtin_amdgcn_fdot2(w, s, eights[g], false);
+          p[2 * i + r] = __builtin_bit_cast(uint32_t, ws);
         }
       }
-      asm volatile("" : "+v"(offset[g]));
-      return p;
+      asm volatile("" : "+v"(offset[g]), "+v"(eights[g]));
+      return __builtin_bit_cast(f16x8, p);
     };
     __builtin_amdgcn_s_setprio(1);  // the part with most products first
     weights(0, 0);
@@ -497,6 +513,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
         const float f = ldexpf(1.0f, vexp - exponent_now);
         vexp = exponent_now;
         #pragma unroll
+        for (int g = 0; g < NG; ++g) eights[g] *= f;
+        #pragma unroll
         for (int d = 0; d < DT; ++d) o[d] *= f;
       }
       work(buf, tile, have, poison);
@@ -517,9 +535,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
   // 4 d + i; two chunks change halves, so that a lane has the 8 channels of one
   const float sum = pair_sum(weight_sum);
   const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
-  const float factor = ldexpf(1.0f, 24 - 14 + vexp);
+  const float factor = ldexpf(1.0f, 24 - kScaleBits + vexp);
   #pragma unroll
-  for (int g = 0; g < NG; ++g) offset[g] = pair_sum(offset[g]);
+  for (int g = 0; g < NG; ++g)
+    offset[g] = pair_sum(fmaf(eights[g], ldexpf(8.0f, vexp - kScaleBits), offset[g]));
   const bool partial = unit.ranges > 1;
   if (partial && unit.slot >= part.slots) return;  // no batch that comet.h allows
   const long long at =
