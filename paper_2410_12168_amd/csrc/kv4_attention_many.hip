@@ -394,6 +394,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
     f16x8 v[DT];
     #pragma unroll
     for (int d = 0; d < DT; ++d) v[d] = v_operand(0, d);
+    u32x4 pairs[2];  // V's {s, mn} of the next operand
+    auto load_pairs = [&](int st, int g) {
+      #pragma unroll
+      for (int i = 0; i < 2; ++i)
+        pairs[i] = *reinterpret_cast<const u32x4*>(params + (2 * g + 1) * kTile + 16 * st +
+                                                   8 * i + 4 * half);
+    };
+    load_pairs(0, 0);
     __builtin_amdgcn_sched_barrier(0);
     const bool whole = have == ~0ull && t0 + kTile - 1 <= wave_pos0 &&
                        (u.window == 0 || t0 > wave_pos1 - u.window);
@@ -443,8 +451,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
       u32x4 p;
       #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const float* at = params + (2 * g + 1) * kTile + 16 * st + 8 * i + 4 * half;
-        const u32x4 v = *reinterpret_cast<const u32x4*>(at);
+        const u32x4 v = pairs[i];
         #pragma unroll
         for (int r = 0; r < 2; ++r) {
           const uint32_t sr = v[r], mr = v[2 + r];
@@ -470,6 +477,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
         #pragma unroll
         for (int d = g * DT / NG; d < (g + 1) * DT / NG; ++d) {
           __builtin_amdgcn_sched_barrier(0);
+          if (d == g * DT / NG) {
+            if (g + 1 < NG)
+              load_pairs(st, g + 1);
+            else if (st < 3)
+              load_pairs(st + 1, 0);
+          }
           o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[d], p, o[d], 0, 0, 0);
           if (st < 3) {
             v[d] = v_operand(st + 1, d);
