@@ -111,7 +111,7 @@ __device__ inline unsigned long long seen_tokens(int pos, int t, int window,
 
 struct UnitShape {
   int group;      // q heads per kv head
-  int rows;       // q rows (of all heads of a group) per block
+  int rows;       // q rows (of all heads of a group) per block, a power of two
   int window;
   int target;     // token ranges to aim at, per kv head
   int at_once;    // units that are at work at the same time, per kv head
@@ -136,7 +136,7 @@ __device__ inline SeqWork seq_work(const PagedBatch& b, int page_shift, const Un
   const int seen = max(0, min(w.len, b.max_pages << page_shift));  // 2^30 at most
   const int low = w.len - w.n - u.window + 1;                       // of the first row's window
   const uint32_t all = (uint32_t)w.n * u.group;
-  w.blocks = (int)all > u.low && (int)all <= u.high ? (all + u.rows - 1) / u.rows : 0;
+  w.blocks = (int)all > u.low && (int)all <= u.high ? (all + u.rows - 1) >> (31 - __clz(u.rows)) : 0;
   w.first = u.window > 0 ? max(0, low) / kTile : 0;
   w.tiles = max(1, (seen + kTile - 1) / kTile - (int)w.first);
   return w;
@@ -169,11 +169,10 @@ __device__ inline uint32_t ranges_of(const SeqWork& w, float per) {
 // ranges of full length are `target` at most (rounded up by more than the 32-bit
 // sum can be off), then where the unit is.  Shorter last ranges can make that more
 // units than run at once, and the device waits for a second turn of a few: ranges up
-// to half as long again are then tried (64 users of 4096 tokens, 64 over 8 heads of
-// 128: 60 us without, 53 with; 32 users of up to 8192: 44 and 41; 0.2 us for batches
-// that do not need it).  Sums of 32 bits: more than a launch
-// can have only in batches that the interface does not allow, whose units are then
-// any or none of the batch's.
+// to half as long again are then tried (64 users of 4096 tokens, 64 heads over 8 of
+// 128 channels: 60 us without, 53 with; 32 users of up to 8192: 44 and 41).  Sums of
+// 32 bits: more than a launch can have only in batches that the interface does not
+// allow, whose units are then any or none of the batch's.
 template <bool SPLIT>
 __device__ inline bool find_unit(const PagedBatch& b, int page_shift, const UnitShape& u,
                                  uint32_t index, Unit* out) {
@@ -190,16 +189,18 @@ __device__ inline bool find_unit(const PagedBatch& b, int page_shift, const Unit
   uint32_t first_upto = sum_upto(start.blocks * first_ranges);
   if (__builtin_expect(from_lane(first_upto, 63) > (uint32_t)u.at_once && b.B <= 64, 0)) {
     const float step = ceilf(per * 0.125f);
-    // not unrolled, and out of the way: most launches skip it
-    #pragma unroll 1
-    for (int i = 1; i <= 4; ++i) {
-      const uint32_t ranges = ranges_of(start, per + i * step);
-      const uint32_t upto = sum_upto(start.blocks * ranges);
-      if (from_lane(upto, 63) <= (uint32_t)u.at_once) {
-        first_ranges = ranges;
-        first_upto = upto;
-        break;
-      }
+    auto fits = [&](float longer, uint32_t* ranges, uint32_t* upto) {
+      *ranges = ranges_of(start, longer);
+      *upto = sum_upto(start.blocks * *ranges);
+      return from_lane(*upto, 63) <= (uint32_t)u.at_once;
+    };
+    uint32_t ranges, upto;
+    if (fits(per + 4 * step, &ranges, &upto)) {  // the longest first: mostly none does
+      int i = 1;
+      #pragma unroll 1
+      while (!fits(per + i * step, &ranges, &upto) && i < 4) ++i;
+      first_ranges = ranges;
+      first_upto = upto;
     }
   }
   uint32_t before = 0, slots_before = 0;
