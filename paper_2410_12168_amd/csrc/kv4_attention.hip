@@ -41,8 +41,8 @@
 // number of tiles, about `target` ranges in all, and a second kernel adds up the
 // ranges of a sequence that has more than one.
 //
-// What bounds it (64 q heads over 8 of 128 channels where nothing else is said; event
-// times of a call, floors at the 4.9 TB/s of a large copy):
+// What bounds it (64 q heads over 8 of 128 channels where nothing else is said; times
+// of a call, passes back to back, floors at the 4.9 TB/s of a large copy):
 //   - 64 users of up to 8192 tokens (284 MB): 74 us, 3.8 TB/s, floor 57.  The waves
 //     wait for the cache: each has the next tile's codes in flight, three blocks on a
 //     compute unit, and the last blocks end alone.  Two thirds or twice the token
@@ -50,8 +50,8 @@
 //   - one user of 131072 tokens, 32 heads (143 MB): 39 us, 3.6 TB/s, floor 29, of which
 //     the sum over 96 ranges and the launches are 8.  Fewer or more ranges: 37 us
 //     with two thirds, 44 with 4/3.
-//   - one user of 100 tokens: 7 us, latency: two tiles a wave at most, but a table, a
-//     tile and a row of q to fetch one after the other, then the waves' sums.
+//   - one user of 100 tokens: 7 us, latency: one tile a wave at most, but the lengths,
+//     the table and a tile to fetch one after the other, then the waves' sums.
 //   - 16 users with 5 drafted rows each, 12 heads of 64 channels, up to 2000 tokens:
 //     16 us (floor 3), 12 of it this kernel and 5 the sum over ranges.
 #include <algorithm>

@@ -18,8 +18,16 @@
 //     turns them.
 //   - 16-byte chunks of a row in LDS change places with the row's number, so that
 //     the reads and writes of 16 lanes meet all banks.
-//   - V's codes count around 8 (c - 8 is as exact, and the offsets are those of code
-//     8), which takes most of the weights' rounding away.
+//   - the weights are fp16 pairs, and everything that they multiply is (scales and
+//     offsets of V) or counts (their sum): two to an operation, with 32-bit sums.  The
+//     sums all go by the same rounded weights.  A weight is scaled by 2^6, a scale of V
+//     by a power of two that puts the largest so far into [2^8, 2^9): their product stays
+//     below 2^15, a weight keeps its 11 bits down to 2^-20 of the largest and is not lost
+//     before 2^-30, a scale down to 2^-22 of the largest.  The product of the two is
+//     rounded once more.  (With weights in 32 bits until that product: a chunk of 512
+//     rows 366 us, now 357.)
+//   - V's codes count around 8 (c - 8 is as exact), 8 w s is added apart: that takes
+//     most of the products' rounding away.
 //
 // 128 rows to a block: with 256 (eight waves) a chunk of 512 rows ran 2.5% faster, but
 // ragged prompts of 2048 rows 6% slower: larger blocks work on more masked tokens, and
@@ -29,14 +37,15 @@
 // fill the end.
 //
 // Bound by the issue of vector operations: per wave and tile of 32 rows x 64 tokens 34
-// products, about 400 other vector operations and 32 exponentials share a SIMD's issue
+// products, about 310 other vector operations and 32 exponentials share a SIMD's issue
 // with the second block's wave (measured: 4 products 62 ns, 32 multiply-adds 78, both
-// together 94).  Vector operations issue in 63% of the cycles, the matrix core works in
-// 33%.  A chunk of 512 rows over 16384 tokens, 64 heads of 128 channels (270 GFLOP):
-// 350 to 365 us, 740 to 770 TFLOP/s; a large fp16 library product reaches 1307.  Prompts
-// of up to 2048 rows, four of them, 32 heads: 129 us.  Not kept, as 1 to 5% slower: the
-// weights' sum by a product with a row of ones, scaling and conversion of the weights
-// in one operation, the score products of both halves interleaved, s_setprio around the
+// together 94).  Vector operations issue in 62% of the cycles, the matrix core works in
+// 38%.  A chunk of 512 rows over 16384 tokens, 64 heads of 128 channels (270 GFLOP):
+// 355 to 363 us, 750 to 763 TFLOP/s; a large fp16 library product reaches 1307.  Prompts
+// of up to 2048 rows, four of them, 32 heads, 64-channel groups: 123 us.  Not kept, as 1
+// to 5% slower: the weights' sum by a product with a row of ones, scaling and conversion
+// of the weights in one operation, the score products of both halves interleaved, the
+// first half's scores next to the second's products (registers), s_setprio around the
 // score products, blocks in order of their length over all sequences.
 #include "attention.h"
 
