@@ -102,14 +102,16 @@ class Paged:
                                                self.params[i][page, :, p % self.page], self.G)
         return out
 
-    def attention(self, q16, H, scale, window=0):
+    def attention(self, q16, H, scale, window=0, rows=None):
         """(out, bound) fp64 [M][H][D]; bound: what fp16 weights and output and fp32 sums may
-        be off by, element by element."""
+        be off by, element by element.  rows: only these (others zero)."""
         q = f64(q16)
         out, bound = (np.zeros((self.M, H, self.D)) for _ in range(2))
         R = H // self.kvh
         cached = {}
         for m, b, p in self.rows():
+            if rows is not None and m not in rows:
+                continue
             lo = max(0, p - window + 1) if window else 0
             js = [j for j in range(lo, p + 1) if self.page_of(b, j) >= 0]
             if not js:

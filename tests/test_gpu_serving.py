@@ -310,6 +310,37 @@ def test_more_sequences_than_lanes_of_a_wave(window):
     check_attention(host16(out), ref, bound)
 
 
+@pytest.mark.parametrize("n,window", [(5, 0), (8, 100), (15, 0), (15, 70)])
+@pytest.mark.parametrize("D,G", [(64, 32), (64, 64), (128, 32), (128, 64), (128, 128)])
+def test_attention_of_many_short_runs_of_rows(D, G, n, window):
+    # sequences enough for blocks of 32 rows (20, 32 and 60 rows of a head's group), some with
+    # fewer rows or none, of one range and of several
+    seqs = [((n, n, 1, n, 0, n)[b % 6], 20 + n + 90 * b) for b in range(12)]
+    p = Paged(D + G + n + window, seqs, 8, D, G, 32)
+    cache, batch = handles(p, max_rows=n)
+    q16 = to16(p.rng.standard_normal((p.M, 32, D)))
+    out = comet.kv4_attention(dev16(q16), cache, batch, window=window)
+    some = p.rng.choice(p.M, 16, replace=False)
+    ref, bound = p.attention(q16, 32, D ** -0.5, window, some)
+    check_attention(host16(out)[some], ref[some], bound[some])
+
+
+@pytest.mark.parametrize("n,H,D,G", [(1, 8, 64, 64), (1, 8, 128, 128), (1, 16, 128, 32),
+                                     (16, 64, 64, 64)])
+def test_attention_of_sequences_just_longer_than_a_range(n, H, D, G):
+    # 9 tiles each and about 2 / 3 of the ranges that run at once: two ranges to a sequence would
+    # be more than that, so a sequence stays whole; a few shorter and longer ones
+    B = 60 if n == 1 else 40
+    seqs = [(n, (576, 570, 576, 100, 576, 640)[b % 6] if b else 900) for b in range(B)]
+    p = Paged(47 + n + D, seqs, 8, D, G, 64)
+    cache, batch = handles(p, max_rows=n)
+    q16 = to16(p.rng.standard_normal((p.M, H, D)))
+    out = comet.kv4_attention(dev16(q16), cache, batch)
+    some = p.rng.choice(p.M, min(p.M, 24), replace=False)
+    ref, bound = p.attention(q16, H, D ** -0.5, rows=some)
+    check_attention(host16(out)[some], ref[some], bound[some])
+
+
 def test_any_device_contents_stay_within_the_buffers():
     """Row starts that fall, negative lengths and lengths beyond the table, pages out of range:
     the calls end, and write nothing outside the rows and the cache.  (All indexes are
