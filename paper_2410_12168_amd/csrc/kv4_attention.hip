@@ -772,8 +772,9 @@ Partials partials_at(float* at, const PagedCache& c, const Part& p) {
 
 // The sum over ranges: blocks for the row blocks that may have several (half the slots
 // at most, and no more than there are), times kv heads, and how many of a row block's
-// rows each takes, so that there are about 2048 in all (each looks its unit up, which
-// costs more than some rows one after the other).
+// rows each takes, so that there are about 1024 in all: each looks its unit up, which
+// costs more than some rows one after the other (64 users of 8192 tokens 4.9 us, with
+// 2048 blocks 6.3, with 4096 10.6; a chunk of 512 rows 12.4 us, with 512 blocks 13.2).
 struct Split {
   unsigned blocks = 0, parts = 0;
   int rows = 1;
@@ -783,7 +784,7 @@ Split split_of(const PagedCache& c, const Part& p) {
   Split s;
   s.blocks = (unsigned)(std::min(p.slots / 2, p.row_blocks) * c.kv_heads);
   if (!s.blocks) return s;
-  s.parts = std::max(1u, std::min((unsigned)p.most_rows, 2048u / s.blocks));
+  s.parts = std::max(1u, std::min((unsigned)p.most_rows, 1024u / s.blocks));
   s.rows = (p.most_rows + s.parts - 1) / s.parts;
   const int at_once = 1024 / c.head_dim;  // rows that a block takes, with few ranges
   if (s.rows > at_once) {
