@@ -43,7 +43,7 @@
 //
 // What bounds it (64 q heads over 8 of 128 channels where nothing else is said; times
 // of a call, passes back to back, floors at the 4.9 TB/s of a large copy):
-//   - 64 users of up to 8192 tokens (284 MB): 74 us, 3.8 TB/s, floor 57.  The waves
+//   - 64 users of up to 8192 tokens (284 MB): 73 us, 3.9 TB/s, floor 57.  The waves
 //     wait for the cache: each has the next tile's codes in flight, three blocks on a
 //     compute unit, and the last blocks end alone.  Two thirds or twice the token
 //     ranges run within 2%.
@@ -53,7 +53,7 @@
 //   - one user of 100 tokens: 7 us, latency: one tile a wave at most, but the lengths,
 //     the table and a tile to fetch one after the other, then the waves' sums.
 //   - 16 users with 5 drafted rows each, 12 heads of 64 channels, up to 2000 tokens:
-//     16 us (floor 3), 12 of it this kernel and 5 the sum over ranges.
+//     16 us (floor 3), 12 of it this kernel and 4 the sum over ranges.
 #include <algorithm>
 
 #include "attention.h"

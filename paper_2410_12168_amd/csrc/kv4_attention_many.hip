@@ -37,12 +37,12 @@
 // fill the end.
 //
 // Bound by the issue of vector operations: per wave and tile of 32 rows x 64 tokens 34
-// products, about 310 other vector operations and 32 exponentials share a SIMD's issue
+// products, about 345 other vector operations and 32 exponentials share a SIMD's issue
 // with the second block's wave (measured: 4 products 62 ns, 32 multiply-adds 78, both
 // together 94).  Vector operations issue in 62% of the cycles, the matrix core works in
 // 38%.  A chunk of 512 rows over 16384 tokens, 64 heads of 128 channels (270 GFLOP):
-// 355 to 363 us, 750 to 763 TFLOP/s; a large fp16 library product reaches 1307.  Prompts
-// of up to 2048 rows, four of them, 32 heads, 64-channel groups: 123 us.  Not kept, as 1
+// 349 to 361 us, 750 to 776 TFLOP/s; a large fp16 library product reaches 1307.  Prompts
+// of up to 2048 rows, four of them, 32 heads, 64-channel groups: 122 us.  Not kept, as 1
 // to 5% slower: the weights' sum by a product with a row of ones, scaling and conversion
 // of the weights in one operation, the score products of both halves interleaved, the
 // first half's scores next to the second's products (registers), s_setprio around the
