@@ -227,6 +227,27 @@ def test_cache_beyond_32_bits():
     check_attention(host16(out), ref, bound)
 
 
+@pytest.mark.parametrize("n,B", [(130, 1), (8, 9)])
+def test_attention_in_a_cache_beyond_32_bits(n, B):
+    # many rows, and few in blocks of 32
+    page, kvh, D, H = 1024, 8, 128, 32
+    cache = comet.KV4Cache.empty(8300, page, kvh, D)
+    p = Paged(50 + n, [(n, 300 + 130 * b) for b in range(B)], kvh, D, 128, page, spare=0)
+    p2 = p.num_pages
+    last = slice(8300 - p2, 8300)
+    for t, a in ((cache.k_codes, p.codes[0]), (cache.v_codes, p.codes[1])):
+        t[last] = dev(a)
+    for t, a in ((cache.k_params, p.params[0]), (cache.v_params, p.params[1])):
+        t[last] = dev16(a)
+    table = np.where(p.table >= 0, p.table + (8300 - p2), -1).astype(np.int32)
+    batch = comet.KV4Batch(dev(p.row_start), dev(p.lens), dev(table), p.M, n)
+    q16 = to16(p.rng.standard_normal((p.M, H, D)))
+    out = comet.kv4_attention(dev16(q16), cache, batch)
+    some = p.rng.choice(p.M, 20, replace=False)
+    ref, bound = p.attention(q16, H, D ** -0.5, rows=some)
+    check_attention(host16(out)[some], ref[some], bound[some])
+
+
 def test_more_sequences_than_a_block_has_lanes():
     n = 1500
     seqs = [(1 if b % 3 else 0, 1 + b % 40) for b in range(n)]
