@@ -65,12 +65,12 @@ namespace {
 // ---- the products --------------------------------------------------------------
 
 // Blocks that a compute unit holds at a time, as the registers allow.
-__host__ __device__ constexpr int resident_few(int D, int C) {
-  return (C == 1 ? 3 : 2) + (D == 64 ? 1 : 0);
+__host__ __device__ constexpr int resident_few(int D, int G, int C) {
+  return (C == 1 ? 3 : 2) + (D == 64 && (C == 1 || G == 64) ? 1 : 0);
 }
 
 template <int D, int G, int C>
-__global__ __launch_bounds__(64 * kWaves, resident_few(D, C)) void kv4_attention_few_kernel(
+__global__ __launch_bounds__(64 * kWaves, resident_few(D, G, C)) void kv4_attention_few_kernel(
     PagedCache c, PagedBatch b, AttentionArgs a, UnitShape u, Partials part) {
   constexpr int NG = D / G;         // groups of a head
   constexpr int KS = D / 32;        // steps of the score product
@@ -684,15 +684,20 @@ __global__ __launch_bounds__(256) void kv4_attention_combine_kernel(PagedCache c
 
 // ---- host ------------------------------------------------------------------------
 
-// Sequences of up to this many q rows (rows times heads of a group) run on the kernel
+// Sequences of up to kFewRows q rows (rows times heads of a group) run on the kernel
 // above, the others on the kernel for many rows, whose 128 rows to a block are then
-// used by half at least; `narrow`: the launch's row blocks are fewer than half the
-// compute units, and the split along the tokens fills the device.  Here and there, us:
+// used by half at least.  Here and there, us:
 //   64 rows of 64 users, 2048 tokens   69   92      96 rows of them   99   96
 //   64 rows of 16 users, 4096 tokens   43   58      96 rows of them   58   63
-//   64 rows of one user, 16384 tokens  21   28      96 rows           24   29
-//   (32-channel groups, 96 rows of 64 users 162 and 148, of one user 34 and 37)
-int most_few(bool narrow) { return narrow ? 96 : 64; }
+//   (32-channel groups, 96 rows of 64 users 162 and 148)
+// In narrow launches, whose blocks of 16 rows are fewer than two fifths of the compute
+// units, all do: the split along the tokens fills the device, and shorter blocks are
+// done sooner.  One user, 8 kv heads:
+//   128 rows, 1024 tokens  11.5  19.5     16384 tokens  29.2  31.7
+//   192 rows               12.8  19.5                   35.3  40.2
+//   (32-channel groups     15.3  24.5                   52.3  53.0)
+//   240 rows: no more      13.3  19.6                   44.0  42.6
+constexpr int kFewRows = 64;
 constexpr int kAny = 0x7FFFFFFF;
 
 // What one of the two kernels does of a batch.
@@ -739,9 +744,9 @@ struct Shape {
 
 Shape shape_of(const PagedCache& c, const PagedBatch& b, int heads, int window, int cus) {
   const long long most = (long long)b.max_rows * (heads / c.kv_heads), blocks16 = (most + 15) / 16;
-  const bool narrow = 2 * std::min(b.B, b.M) * blocks16 * c.kv_heads < cus;
+  const bool narrow = 5 * std::min(b.B, b.M) * blocks16 * c.kv_heads < 2 * cus;
   Shape s;
-  s.any_many = most > most_few(narrow);
+  s.any_many = !narrow && most > kFewRows;
   // Sequences of few rows among others get a launch of their own, except where most
   // sequences must have about as many rows as the longest: the launch costs 4 us where
   // no sequence is for it (8 prompts of 512 rows: 348 and 344 us without), the kernel for
@@ -754,11 +759,11 @@ Shape shape_of(const PagedCache& c, const PagedBatch& b, int heads, int window, 
   // 32 rows 17.6 and 19.5), and not next to sequences of many rows, where few rows are
   // mostly one token's (64 users of 8192, 32-channel groups, 8 rows: 167 and 210)
   s.columns = s.any_many || narrow || blocks16 % 2 ? 1 : 2;
-  s.few = part_of(c, b, heads, window, cus, 16 * s.columns, resident_few(128, s.columns),
-                  resident_few(c.head_dim, s.columns), 0,
-                  s.any_many ? most_few(narrow) : kAny);
+  s.few = part_of(c, b, heads, window, cus, 16 * s.columns,
+                  resident_few(128, 128, s.columns), resident_few(c.head_dim, c.G, s.columns), 0,
+                  s.any_many ? kFewRows : kAny);
   s.many = part_of(c, b, heads, window, cus, kManyRows, 2, 2,
-                   s.any_few ? most_few(narrow) : 0, kAny);
+                   s.any_few ? kFewRows : 0, kAny);
   return s;
 }
 

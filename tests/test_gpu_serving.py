@@ -331,6 +331,121 @@ def test_more_sequences_than_lanes_of_a_wave(window):
     check_attention(host16(out), ref, bound)
 
 
+# The kernel for many rows: eight heads of K and V, 52 q rows and more to each.
+
+def some_rows(p, rows=12):
+    """The first and the last of each sequence, and others."""
+    ends = np.concatenate([p.row_start[:-1], p.row_start[1:] - 1])
+    return np.unique(np.concatenate([ends[(ends >= 0) & (ends < p.M)],
+                                     p.rng.choice(p.M, rows, replace=False)]))
+
+
+@pytest.mark.parametrize("window", [0, 90])
+@pytest.mark.parametrize("page", [16, 128])
+@pytest.mark.parametrize("D,G", [(64, 32), (64, 64), (128, 32), (128, 64), (128, 128)])
+def test_many_rows_in_every_form(D, G, page, window):
+    p = Paged(D + G + page + window, [(100, 250), (1, 40), (75, 75), (130, 700)], 8, D, G, page)
+    cache, batch = handles(p, max_rows=130)
+    q16 = to16(p.rng.standard_normal((p.M, 32, D)))
+    out = host16(comet.kv4_attention(dev16(q16), cache, batch, window=window))
+    some = some_rows(p)
+    ref, bound = p.attention(q16, 32, D ** -0.5, window, some)
+    check_attention(out[some], ref[some], bound[some])
+
+
+def test_many_rows_around_holes():
+    seqs = [(40, 200), (40, 100), (40, 150)]
+    holes = [(0, 0), (0, 5), (0, 12), (2, 3), (2, 4), (2, 5), (2, 6), (2, 7)] + [
+        (1, j) for j in range(7)]
+    p = Paged(55, seqs, 8, 128, 64, 16, holes=holes)
+    cache, batch = handles(p, max_rows=40)
+    q16 = to16(p.rng.standard_normal((p.M, 32, 128)))
+    out = host16(comet.kv4_attention(dev16(q16), cache, batch))
+    some = some_rows(p)
+    ref, bound = p.attention(q16, 32, 128 ** -0.5, rows=some)
+    check_attention(out[some], ref[some], bound[some])
+    assert not out[40:80].any()
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.3, 2.0])
+def test_many_rows_with_scales(scale):
+    p = Paged(57, [(60, 150), (60, 17)], 8, 64, 64, 32)  # the second has rows without a token
+    cache, batch = handles(p, max_rows=60)
+    q16 = to16(0.3 * p.rng.standard_normal((p.M, 32, 64)))
+    out = host16(comet.kv4_attention(dev16(q16), cache, batch, scale=scale))
+    some = some_rows(p)
+    ref, bound = p.attention(q16, 32, scale, rows=some)
+    check_attention(out[some], ref[some], bound[some])
+    assert not out[60:60 + 43].any()
+
+
+@pytest.mark.parametrize("kind", ["large", "small", "mixed", "zero"])
+def test_many_extreme_rows(kind):
+    n, L, kvh, H = 60, 180, 8, 32
+    p = Paged(59, [(n, L)], kvh, 128, 64, 16)
+    rng = p.rng
+    size = {"large": np.full(L, 2e4), "small": np.full(L, 1e-6), "zero": np.zeros(L),
+            "mixed": np.where(np.arange(L) % 7 == 0, 1e3, 1e-3)}[kind]
+    for i in (0, 1):
+        rows = np.clip(rng.standard_normal((L, kvh, 128)), -3, 3) * size[:, None, None]
+        if i == 0 and kind == "mixed":
+            rows *= 1e-3
+        c, prm = oracle.kv4_quantize(to16(rows).reshape(L * kvh, 128), 64)
+        p.store(i, 0, np.arange(L), c.reshape(L, kvh, -1), prm.reshape(L, kvh, 2, 2))
+    cache, batch = handles(p)
+    q16 = to16(rng.standard_normal((n, H, 128)) * {"large": 1e-5, "small": 1e4}.get(kind, 1.0))
+    out = host16(comet.kv4_attention(dev16(q16), cache, batch))
+    some = some_rows(p)
+    ref, bound = p.attention(q16, H, 128 ** -0.5, rows=some)
+    check_attention(out[some], ref[some], bound[some], kind)
+
+
+def test_what_many_rows_do_not_see_does_not_reach_them():
+    n, window = 60, 30
+    p = Paged(61, [(n, 100)], 8, 64, 64, 16)
+    q16 = to16(p.rng.standard_normal((n, 32, 64)))
+    ref, bound = p.attention(q16, 32, 0.125, window)
+    for i in (0, 1):
+        for j, bits in ((99, 0x7E00), (60, 0x7C00)):
+            p.params[i][p.page_of(0, j), :, j % 16] = bits
+    cache, batch = handles(p)
+    bad = q16.copy()
+    bad[0, 0, 5] = 0x7C00
+    bad[0, 2, 6] = 0x7E00
+    out = host16(comet.kv4_attention(dev16(bad), cache, batch, window=window))
+    at = np.arange(100 - n, 100)
+    blind = (at < 99) & ~((at >= 60) & (at - window < 60))
+    assert blind[0] and 2 <= blind.sum() < n - 1
+    others = [h for h in range(32) if h not in (0, 2)]
+    check_attention(out[0, others], ref[0, others], bound[0, others])
+    assert np.isnan(f64(out[~blind])).all()
+    blind[0] = False
+    check_attention(out[blind], ref[blind], bound[blind])
+
+
+def test_many_rows_captured_and_replayed():
+    p = Paged(63, [(60, 400), (1, 300), (90, 90), (20, 900)], 8, 128, 128, 64)
+    cache, batch = handles(p, max_rows=90)
+    q = dev16(to16(p.rng.standard_normal((p.M, 32, 128))))
+    out = torch.empty_like(q)
+    workspace = comet.kv4_attention_workspace(q, cache, batch)
+    call = lambda: comet.kv4_attention(q, cache, batch, out=out, workspace=workspace)  # noqa: E731
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    lens = batch.seq_lens.clone()
+    for step in range(4):
+        batch.seq_lens.copy_(lens - 11 * step)
+        q.mul_(1.0 + 0.125 * step)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone()
+        call()
+        assert torch.equal(got.view(torch.int16), out.view(torch.int16)), step
+
+
 @pytest.mark.parametrize("n,window", [(5, 0), (8, 100), (15, 0), (15, 70)])
 @pytest.mark.parametrize("D,G", [(64, 32), (64, 64), (128, 32), (128, 64), (128, 128)])
 def test_attention_of_many_short_runs_of_rows(D, G, n, window):
