@@ -309,8 +309,8 @@ def test_attention(seqs, H, kvh, D, G, page, window):
 @pytest.mark.parametrize("n", [1, 20, 100])
 @pytest.mark.parametrize("D,G", [(64, 32), (64, 64), (128, 32), (128, 64), (128, 128)])
 def test_attention_in_every_form(D, G, n, page):
-    # few rows in blocks of 16 and of 32, many rows; tiles within a page and over several;
-    # one range and several
+    # blocks of 16 rows, one and several; tiles within a page and over several; one range and
+    # several
     p = Paged(D + G + n + page, [(n, 150 + n), (1, 40), (n, 700)], 2, D, G, page)
     cache, batch = handles(p, max_rows=n)
     q16 = to16(p.rng.standard_normal((p.M, 4, D)))
