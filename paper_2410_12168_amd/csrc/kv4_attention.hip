@@ -18,6 +18,11 @@
 //     operand takes back.  The order within a dword is (0, 4, 1, 5, 2, 6, 3, 7).
 //   - q is scaled by a power of two per row (largest value in [2^10, 2^11)), so
 //     that neither that factor nor subnormals cost bits.
+//   - scale * log2(e) is a mantissa, multiplied into K's scales and the sums of q, times
+//     a power of two that turns a score into the exponent of its weight (`kappa`).  That
+//     product is exact, so that the largest score's exponent is 0 and none is above it,
+//     however large the scores: with the whole factor in it, a rounded maximum of 2^24
+//     and more left exponents above 0, and weights beyond fp16.
 //   - w_j s_j is scaled by a power of two per wave, so that the largest scale of
 //     the tokens so far lands in [2^14, 2^15): a weight loses bits only where it
 //     is 2^-28 of the largest.  It is rounded to fp16 (2^-11 relative).
@@ -55,6 +60,7 @@
 //   - 16 users with 5 drafted rows each, 12 heads of 64 channels, up to 2000 tokens:
 //     16 us (floor 3), 12 of it this kernel and 4 the sum over ranges.
 #include <algorithm>
+#include <cmath>
 
 #include "attention.h"
 
@@ -225,7 +231,7 @@ __global__ __launch_bounds__(64 * kWaves, resident_few(D, G, C)) void kv4_attent
     if (big > 0.0f && big < INFINITY) e = ilogbf(big);
     const float f = ldexpf(a.scale < 0.0f ? -1.0f : 1.0f, 10 - e);
     // above 0, so that an unseen token's -infinity stays one
-    kappa[cb] = fmaxf(ldexpf(fabsf(a.scale) * kLog2e, 24 + e - 10), 0x1p-120f);
+    kappa[cb] = fmaxf(ldexpf(1.0f, a.exponent + 24 + e - 10), 0x1p-120f);
     #pragma unroll
     for (int g = 0; g < NG; ++g) qsum[cb][g] = 0.0f;
     #pragma unroll
@@ -245,7 +251,7 @@ __global__ __launch_bounds__(64 * kWaves, resident_few(D, G, C)) void kv4_attent
                        (_Float16)(v[3] * 0.0625f), (_Float16)(v[7] * 0.0625f)};
     }
     #pragma unroll
-    for (int g = 0; g < NG; ++g) qsum[cb][g] = quad_sum(qsum[cb][g]) * 0x1p-24f;
+    for (int g = 0; g < NG; ++g) qsum[cb][g] = quad_sum(qsum[cb][g]) * (0x1p-24f * a.mantissa);
     top[cb] = kNone;
     weight_sum[cb] = 0.0f;
     #pragma unroll
@@ -466,7 +472,7 @@ __global__ __launch_bounds__(64 * kWaves, resident_few(D, G, C)) void kv4_attent
     #pragma unroll
     for (int g = 0; g < NG; ++g) {
       float* at = params + 4 * g * kTile + lane;
-      at[0] = low_half(preg[0][g]);
+      at[0] = low_half(preg[0][g]) * a.mantissa;
       at[kTile] = low_half(preg[0][g] >> 16);
       at[2 * kTile] = low_half(preg[1][g]) * weight_unit;
       at[3 * kTile] = fmaf(8.0f, low_half(preg[1][g]), low_half(preg[1][g] >> 16));  // of code 8
@@ -827,8 +833,10 @@ size_t attention_workspace(const PagedCache& c, const PagedBatch& b, int heads, 
                           (s.any_many ? partial_floats(c, s.many) : 0));
 }
 
-hipError_t launch_kv4_attention(const PagedCache& c, const PagedBatch& b, const AttentionArgs& a,
+hipError_t launch_kv4_attention(const PagedCache& c, const PagedBatch& b, const AttentionArgs& args,
                                 hipStream_t stream) {
+  AttentionArgs a = args;
+  a.mantissa = std::frexp(std::fabs(a.scale) * kLog2e, &a.exponent);
   const Shape s = shape_of(c, b, a.heads, a.window, a.cus);
   float* ws = static_cast<float*>(a.workspace);
   const Partials few = partials_at(ws, c, s.few);

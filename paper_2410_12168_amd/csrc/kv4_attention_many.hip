@@ -24,7 +24,9 @@
 //     by a power of two that puts the largest so far into [2^8, 2^9): their product stays
 //     below 2^15, a weight keeps its 11 bits down to 2^-20 of the largest and is not lost
 //     before 2^-30, a scale down to 2^-22 of the largest.  The product of the two is
-//     rounded once more.  (With weights in 32 bits until that product: a chunk of 512
+//     rounded once more.  (The 2^6 go into the exponent of a weight, next to the row's
+//     largest score, which has to leave room for them: not so from 2^22 on, where
+//     scores are a quarter apart and more and a weight starts at 1.)  (With weights in 32 bits until that product: a chunk of 512
 //     rows 366 us, now 357.)
 //   - V's codes count around 8 (c - 8 is as exact), 8 w s is added apart: that takes
 //     most of the products' rounding away.
@@ -197,7 +199,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
   if (big > 0.0f && big < INFINITY) e = ilogbf(big);
   const float qf = ldexpf(a.scale < 0.0f ? -1.0f : 1.0f, 10 - e);
   // above 0, so that an unseen token's -infinity stays one
-  const float kappa = fmaxf(ldexpf(fabsf(a.scale) * kLog2e, 8 + e - 10), 0x1p-120f);
+  const float kappa = fmaxf(ldexpf(1.0f, a.exponent + 8 + e - 10), 0x1p-120f);
   #pragma unroll
   for (int g = 0; g < NG; ++g) qsum[g] = offset[g] = eights[g] = 0.0f;
   #pragma unroll
@@ -224,7 +226,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
     f16x8 low = {0, 0, 0, 0, 0, 0, 0, 0}, high = low;  // of the halves of the lanes
     #pragma unroll
     for (int g = 0; g < NG; ++g) {
-      float rest = pair_sum(qsum[g]) * 0x1p-8f;
+      float rest = pair_sum(qsum[g]) * (0x1p-8f * a.mantissa);
       #pragma unroll
       for (int i = 3 * g; i < 3 * g + 3; ++i) {
         const _Float16 part = (_Float16)rest;
@@ -248,6 +250,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
     #pragma unroll
     for (int k = 0; k < 16; ++k) o[d][k] = 0.0f;
   int vexp = -24;  // the exponent below that `o` goes by
+
+  // The exponent of a row's largest weight.
+  auto lift = [](float top) { return fabsf(top) < 0x1p22f ? (float)kWeightBits : 0.0f; };
 
   // Where a 16-byte chunk (8 channels) of a token lies in LDS.
   auto k_place = [](int t, int chunk) {
@@ -308,7 +313,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
     _Float16* v_at = reinterpret_cast<_Float16*>(lds + buf + P_AT) + 8 * (lane >> 2) + (lane & 3);
     #pragma unroll
     for (int g = 0; g < NG; ++g) {
-      if (wave == 0) at[2 * g * kTile] = low_half(preg[0][g]) * 65536.0f;
+      if (wave == 0) at[2 * g * kTile] = low_half(preg[0][g]) * (65536.0f * a.mantissa);
       if (wave == 1)
         v_at[2 * (2 * g + 1) * kTile] = (_Float16)(low_half(preg[1][g]) * scale_unit);
       if (wave == 2)
@@ -428,7 +433,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
     for (int k = 1; k < 32; ++k) m = fmaxf(m, x[k / 16][k % 16]);
     const float next = fmaxf(top, pair_max(m) * kappa);
     if (__any(next > top)) {
-      const float f = __builtin_amdgcn_exp2f(top - next);
+      const float f = __builtin_amdgcn_exp2f(top - next + (lift(next) - lift(top)));
       top = next;
       weight_sum *= f;
       #pragma unroll
@@ -441,7 +446,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
     }
     // the weighted sum, 16 tokens at a time; the weights of the next 16 are worked out
     // next to the products of these
-    const float shift = kWeightBits - top;
+    // one value of `top` from here on: known to be lift's of the branch above on some
+    // paths, it costs 38 spilled registers
+    asm volatile("" : "+v"(top));
+    const float shift = lift(top) - top;
     const f16x2 ones = {1, 1};
     f16x2 wt[2][4];  // of 16 tokens and the next: pairs of the 8 that this half has
     auto weights = [&](int st, int i) {  // of tokens 8 i + 4 half .. + 3 of the 16
@@ -555,12 +563,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
 
   // ---- out: element 4 i + r of half h is channel (0, 4, 1, 5)[r] + 2 h of chunk
   // 4 d + i; two chunks change halves, so that a lane has the 8 channels of one
-  const float sum = pair_sum(weight_sum);
+  const float even = lift(top) != 0.0f ? 1.0f : ldexpf(1.0f, kWeightBits);  // alike in all ranges
+  const float sum = pair_sum(weight_sum) * even;
   const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
-  const float factor = ldexpf(1.0f, 24 - kScaleBits + vexp);
+  const float factor = ldexpf(even, 24 - kScaleBits + vexp);
   #pragma unroll
   for (int g = 0; g < NG; ++g)
-    offset[g] = pair_sum(fmaf(eights[g], ldexpf(8.0f, vexp - kScaleBits), offset[g]));
+    offset[g] = even * pair_sum(fmaf(eights[g], ldexpf(8.0f, vexp - kScaleBits), offset[g]));
   const bool partial = unit.ranges > 1;
   if (partial && unit.slot >= part.slots) return;  // no batch that comet.h allows
   const long long at =

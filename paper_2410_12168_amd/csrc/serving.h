@@ -66,6 +66,9 @@ struct AttentionArgs {
   int window;
   void* workspace;
   int cus;
+  // |scale| * log2(e) as mantissa * 2^exponent, for the kernels (the launcher's own)
+  float mantissa = 0.0f;
+  int exponent = 0;
 };
 // nullptr, or why these sizes cannot run.
 const char* attention_refusal(const PagedCache& c, const PagedBatch& b, int heads, int cus);
