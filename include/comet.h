@@ -344,7 +344,8 @@ COMET_API comet_status_t comet_kv4_gather(const comet_kv4_cache_t* cache,
  *     out = sum_j w_j v_j / sum_j w_j,  w_j = exp(scale * q . k_j),
  * with the k_j and v_j of kv head h / (heads / kv_heads) as q * s + mn of their
  * codes, without the rounding to fp16 of comet_kv4_dequantize.  A row that sees
- * no token is zeros.  Products are exact to fp16 inputs (the weights w_j, and
+ * no token is zeros; one that sees a token is not-a-number where its q has an
+ * infinity or not-a-number.  Products are exact to fp16 inputs (the weights w_j, and
  * those times a scale of V, are rounded to fp16, relative to the largest), sums
  * are fp32, the output is rounded once.  Scales of V below 2^-22 of the largest
  * in a sequence lose bits.  What a row does not see has no influence on it, not-a-number

@@ -229,7 +229,9 @@ __global__ __launch_bounds__(64 * kWaves, resident_few(D, G, C)) void kv4_attent
     big = quad_max(big);
     int e = 10;
     if (big > 0.0f && big < INFINITY) e = ilogbf(big);
-    const float f = ldexpf(a.scale < 0.0f ? -1.0f : 1.0f, 10 - e);
+    // an infinity in q: all scores of the row are infinities or not-a-numbers, and its
+    // weights not-a-numbers, whatever their sign
+    const float f = big < INFINITY ? ldexpf(a.scale < 0.0f ? -1.0f : 1.0f, 10 - e) : NAN;
     // above 0, so that an unseen token's -infinity stays one
     kappa[cb] = fmaxf(ldexpf(1.0f, a.exponent + 24 + e - 10), 0x1p-120f);
     #pragma unroll

@@ -197,7 +197,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
   big = pair_max(big);
   int e = 10;
   if (big > 0.0f && big < INFINITY) e = ilogbf(big);
-  const float qf = ldexpf(a.scale < 0.0f ? -1.0f : 1.0f, 10 - e);
+  // an infinity in q makes the row not-a-number (see kv4_attention.hip)
+  const float qf = big < INFINITY ? ldexpf(a.scale < 0.0f ? -1.0f : 1.0f, 10 - e) : NAN;
   // above 0, so that an unseen token's -infinity stays one
   const float kappa = fmaxf(ldexpf(1.0f, a.exponent + 8 + e - 10), 0x1p-120f);
   #pragma unroll
