@@ -899,6 +899,9 @@ comet_status_t comet_kv4_attention(const comet_kv4_cache_t* cache, const comet_k
   if ((st = check_rows(Q, q_stride, heads, c.head_dim, "Q"))) return st;
   if ((st = check_rows(out, out_stride, heads, c.head_dim, "out"))) return st;
   if (!std::isfinite(scale)) return fail(COMET_ERR_INVALID_ARG, "scale is not finite");
+  // the scores of any finite rows stay within the running maximum's first value
+  if (std::fabs(scale) > 0x1p56f)
+    return fail(COMET_ERR_UNSUPPORTED, "scale=%g exceeds 2^56", (double)scale);
   if (window < 0) return fail(COMET_ERR_INVALID_ARG, "window=%d must be >= 0", window);
   if (!aligned16(workspace))
     return fail(COMET_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
