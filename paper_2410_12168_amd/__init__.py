@@ -336,9 +336,15 @@ class KV4BatchStruct(ctypes.Structure):
         (n, ctypes.c_int) for n in ("B", "M", "max_pages", "max_rows")]
 
 
+_INT_MAX = 2 ** 31 - 1  # larger numbers would lose their upper bits on the way
+
+
 def _row_room(t, M: int, stride: int, width: int, name: str) -> None:
     """A tensor of fp16 rows must reach, from its first element to the end of its
-    storage, over M rows of `width` elements, `stride` apart."""
+    storage, over M rows of `width` elements, `stride` apart; the stride is an int of
+    the interface."""
+    if stride > _INT_MAX:
+        raise ValueError(f"{name}: stride {stride} exceeds 2^31 - 1")
     if t is None or isinstance(t, int):
         return
     have = t.nbytes if isinstance(t, np.ndarray) else (
@@ -384,6 +390,8 @@ def comet_kv4_attention(cache, batch, Q, out, heads: int, q_stride: int, out_str
         if b.M > 0 and heads > 0:
             _row_room(Q, b.M, q_stride, heads * c.head_dim, "Q")
             _row_room(out, b.M, out_stride, heads * c.head_dim, "out")
+    if window > _INT_MAX:
+        raise ValueError(f"window: {window} exceeds 2^31 - 1")
     have = _nbytes(workspace)
     if workspace_bytes is None:
         workspace_bytes = have or 0
@@ -655,8 +663,10 @@ def _heads_of(t, name: str, here: int):
         got = (f"{t.dtype} {tuple(t.shape)} on {t.device}" if isinstance(t, _torch.Tensor)
                else type(t).__name__)
         raise ValueError(f"{name}: need a float16 CUDA tensor [rows][heads][channels], got {got}")
-    if s2 == 1 and s1 == D and s0 >= H * D:
+    if s2 == 1 and s1 == D and H * D <= s0 <= _INT_MAX:
         return M, H, D, s0
+    if M > 1 and s0 > _INT_MAX:
+        raise ValueError(f"{name}: row stride {s0} exceeds 2^31 - 1")
     if (s2 != 1 and D > 1) or (s1 != D and H > 1) or (s0 < H * D and M > 1):
         raise ValueError(f"{name}: heads and channels must be contiguous and rows apart, got "
                          f"strides {t.stride()} for {tuple(t.shape)}")
@@ -784,7 +794,7 @@ class KV4Batch:
             raise ValueError(f"block_table: shape {tuple(block_table.shape)}, expected ({B}, pages)")
         self.row_start, self.seq_lens, self.block_table = row_start, seq_lens, block_table
         self.B, self.M, self.max_pages = B, M, block_table.shape[1]
-        self.max_rows = M if max_rows is None else max_rows
+        self.max_rows = M if max_rows is None else min(max_rows, M)
         self.device = seq_lens.device
         self.struct = KV4BatchStruct(row_start.data_ptr(), seq_lens.data_ptr(),
                                      block_table.data_ptr(), B, M, self.max_pages, self.max_rows)
@@ -884,7 +894,7 @@ def kv4_attention(q, cache: KV4Cache, batch: KV4Batch, scale: Optional[float] = 
         _plain(workspace, "uint8", "workspace", here)
     status = (_lib or lib()).comet_kv4_attention(
         cache.address, batch.address, q.data_ptr(), out.data_ptr(), H, qs, os_,
-        D ** -0.5 if scale is None else scale, window, workspace.data_ptr(), workspace.numel(),
+        D ** -0.5 if scale is None else scale, min(window, _INT_MAX), workspace.data_ptr(), workspace.numel(),
         _stream(stream))
     if status:
         _check(status)

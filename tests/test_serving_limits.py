@@ -16,3 +16,74 @@ def test_scales_whose_scores_pass_the_running_maximum(scale):
     assert 128 * 65504.0 * 16 * 65504.0 * 2.0 ** 56 / math.log(2) < 1e30
     assert attend(cache(), batch(), scale=scale) == 2
     assert "scale" in comet.comet_last_error()
+
+
+# --- numbers that do not fit the 32 bits of the interface --------------------------------
+
+def meta_rows(rows, heads, D, stride):
+    import torch
+
+    comet._need_torch()
+    return torch.empty_strided((rows, heads, D), (stride, D, 1), dtype=torch.float16, device="meta")
+
+
+@pytest.mark.parametrize("stride", [2 ** 31, 2 ** 32 + 128, 2 ** 40])
+def test_row_strides_beyond_32_bits(stride):
+    # the last tokens of sequences of 2^18 in a padded batch, for instance
+    t = meta_rows(2, 1, 64, stride)
+    with pytest.raises(ValueError, match="x: .*stride"):
+        comet._heads_of(t, "x", t.get_device())
+    assert comet._heads_of(meta_rows(1, 1, 64, stride), "x", t.get_device())[3] == 64
+    near = meta_rows(2, 1, 64, 2 ** 31 - 64)
+    assert comet._heads_of(near, "x", t.get_device()) == (2, 1, 64, 2 ** 31 - 64)
+
+
+@pytest.mark.parametrize("stride", [2 ** 31, 2 ** 32 + 512])
+def test_raw_strides_beyond_32_bits(stride):
+    F = 0x10000
+    for call in (lambda: comet.comet_rope(F, F, F, 2 * F, 2, 3, 64, 32, stride, 512, stream=0),
+                 lambda: comet.comet_rope(F, F, F, 2 * F, 2, 3, 64, 32, 512, stride, stream=0),
+                 lambda: comet.comet_kv4_append(cache(), batch(), F, F, stride, 256, stream=0),
+                 lambda: comet.comet_kv4_gather(cache(), batch(), F, F, 256, stride, stream=0),
+                 lambda: comet.comet_kv4_attention(cache(), batch(), F, F, 4, stride, 512, 0.1,
+                                                   stream=0),
+                 lambda: comet.comet_kv4_attention(cache(), batch(), F, F, 4, 512, stride, 0.1,
+                                                   stream=0)):
+        with pytest.raises(ValueError, match="stride"):
+            call()
+
+
+def test_windows_and_row_counts_beyond_32_bits(monkeypatch):
+    F = 0x10000
+    with pytest.raises(ValueError, match="window"):
+        comet.comet_kv4_attention(cache(), batch(), F, F, 4, 512, 512, 0.1, window=2 ** 32 + 5,
+                                  stream=0)
+    # a window that reaches over everything has no effect; no sequence has more rows than there are
+    import torch
+
+    seen = []
+
+    class Library:
+        def comet_kv4_attention(self, *args):
+            seen.append(args)
+            return 0
+
+    class Handle:
+        struct = address = None
+        M, head_dim = 2, 64
+
+    t = meta_rows(2, 4, 64, 256)
+    monkeypatch.setattr(comet, "_lib", Library())
+    monkeypatch.setattr(comet, "_kv4_here", lambda *a: t.get_device())
+    monkeypatch.setattr(comet, "_plain", lambda *a: None)
+    ws = torch.empty(0, dtype=torch.uint8)
+    monkeypatch.setattr(torch.Tensor, "data_ptr", lambda self: F)
+    for window in (2 ** 31 - 1, 2 ** 31, 2 ** 32 + 5, 2 ** 63):
+        comet.kv4_attention(t, Handle, Handle, window=window, out=t, workspace=ws, stream=0)
+        assert seen[-1][8] == 2 ** 31 - 1
+    comet.kv4_attention(t, Handle, Handle, window=7, out=t, workspace=ws, stream=0)
+    assert seen[-1][8] == 7
+    ints = lambda *v: torch.tensor(v, dtype=torch.int32)  # noqa: E731
+    monkeypatch.setattr(comet, "_tensor", lambda *a: None)
+    b = comet.KV4Batch(ints(0, 1, 3), ints(5, 9), ints(0, 1).view(2, 1), 3, 2 ** 32 + 1)
+    assert b.max_rows == b.struct.max_rows == 3
