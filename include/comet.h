@@ -357,7 +357,9 @@ COMET_API comet_status_t comet_kv4_gather(const comet_kv4_cache_t* cache,
  *              (NULL where that is 0): the caller's, for the partial results of
  *              long contexts, needing no initial content and holding none
  *              between calls.  Calls that may overlap need one each.
- * heads a multiple of kv_heads, at most 1024; scale finite, |scale| at most 2^56
+ * heads a multiple of kv_heads, at most 1024; M * heads at most 2^27 and B *
+ * kv_heads at most 2^22 always run (COMET_ERR_UNSUPPORTED somewhere beyond, as the
+ * launches allow); scale finite, |scale| at most 2^56
  * (COMET_ERR_UNSUPPORTED beyond); window >= 0 (0: no limit). */
 COMET_API comet_status_t comet_kv4_attention(const comet_kv4_cache_t* cache,
                                              const comet_kv4_batch_t* batch, const uint16_t* Q,

@@ -87,3 +87,40 @@ def test_windows_and_row_counts_beyond_32_bits(monkeypatch):
     monkeypatch.setattr(comet, "_tensor", lambda *a: None)
     b = comet.KV4Batch(ints(0, 1, 3), ints(5, 9), ints(0, 1).view(2, 1), 3, 2 ** 32 + 1)
     assert b.max_rows == b.struct.max_rows == 3
+
+
+# --- the largest launches ------------------------------------------------------------------
+
+@pytest.fixture(scope="module")
+def shim(tmp_path_factory):
+    return hip_record.library(str(tmp_path_factory.mktemp("hip_record")))
+
+
+def attention_launches(shim, cases):
+    """Per case (kv heads, heads, B, M, max_pages, max_rows): the kernels that a call launches,
+    or why it is refused."""
+    return hip_record.run(shim, f"""
+out = []
+for kvh, heads, B, M, pages, rows in {cases!r}:
+    c = comet.KV4CacheStruct(P, P, P, P, 1 << 20, 16, kvh, 64, 64)
+    b = comet.KV4BatchStruct(P, P, P, B, M, pages, rows)
+    n = comet.comet_kv4_attention_workspace(c, b, heads, 256)
+    try:
+        comet.comet_kv4_attention(c, b, P, P, heads, 64 * heads, 64 * heads, 0.1, 0, P, n, stream=1)
+        out.append([line.split()[2] for line in log()])
+    except comet.CometError as e:
+        out.append([str(e)] + log())
+print(json.dumps(out))
+""")
+
+
+def test_batches_that_always_run(shim):
+    """What comet.h says that is never too large for a launch, at its ends, and beyond."""
+    ends = [(8, 128, 1, (1 << 27) // 128, 1, 1 << 20), (64, 64, 65536, 65536, 1, 1),
+            (64, 1024, 65536, 65536 * 2, 9, 9), (1, 64, 65536, 65535 * 32, 64, 40),
+            (1024, 1024, 4096, 4096 * 32, 5, 32)]
+    for case, kernels in zip(ends, attention_launches(shim, ends)):
+        assert len(kernels) >= 1 and all("kernel" in k for k in kernels), (case, kernels)
+    beyond = [(1024, 1024, 65536, 65536, 1, 1), (8, 1024, 8, 65535 * 32, 64, 1 << 20)]
+    for case, kernels in zip(beyond, attention_launches(shim, beyond)):
+        assert len(kernels) == 1 and "too many rows" in kernels[0], (case, kernels)
