@@ -726,7 +726,18 @@ def rope(x, positions, freqs, interleaved: bool = False, mscale: float = 1.0, ou
     return out
 
 
-class KV4Cache:
+class _Handle:
+    """Tensors and the struct with their addresses.  An attribute is set once: another
+    tensor in its place would not reach the struct, whose address nothing kept alive."""
+
+    def __setattr__(self, name, value):
+        if self.__dict__.get(name, value) is not value:  # (not so in `handle.lens += 1`)
+            raise AttributeError(f"{type(self).__name__}.{name} is fixed: write into its tensor, "
+                                 "or make a new object")
+        self.__dict__[name] = value
+
+
+class KV4Cache(_Handle):
     """A paged 4-bit K/V cache: codes uint8 [num_pages][kv_heads][page_size][head_dim / 2]
     and params float16 [num_pages][kv_heads][page_size][head_dim / G][2] of K and of V,
     contiguous CUDA tensors that this object keeps alive."""
@@ -776,7 +787,7 @@ class KV4Cache:
         return cls(codes[0], params[0], codes[1], params[1])
 
 
-class KV4Batch:
+class KV4Batch(_Handle):
     """The rows of a call and where their sequences lie: row_start int32 [B + 1], seq_lens
     int32 [B], block_table int32 [B][max_pages] (comet_kv4_batch_t), CUDA tensors that this
     object keeps alive; their contents are read when the work runs.  M: rows of the buffers;
@@ -792,13 +803,14 @@ class KV4Batch:
         _exact(row_start, B + 1, "row_start")
         if block_table.dim() != 2 or block_table.shape[0] != B:
             raise ValueError(f"block_table: shape {tuple(block_table.shape)}, expected ({B}, pages)")
-        self.row_start, self.seq_lens, self.block_table = row_start, seq_lens, block_table
-        self.B, self.M, self.max_pages = B, M, block_table.shape[1]
-        self.max_rows = M if max_rows is None else min(max_rows, M)
-        self.device = seq_lens.device
-        self.struct = KV4BatchStruct(row_start.data_ptr(), seq_lens.data_ptr(),
-                                     block_table.data_ptr(), B, M, self.max_pages, self.max_rows)
-        self.address = ctypes.addressof(self.struct)
+        max_pages = block_table.shape[1]
+        max_rows = M if max_rows is None else min(max_rows, M)
+        struct = KV4BatchStruct(row_start.data_ptr(), seq_lens.data_ptr(), block_table.data_ptr(), B,
+                                M, max_pages, max_rows)
+        # at once: a serving program makes one of these per step
+        self.__dict__.update(row_start=row_start, seq_lens=seq_lens, block_table=block_table, B=B,
+                             M=M, max_pages=max_pages, max_rows=max_rows, device=seq_lens.device,
+                             struct=struct, address=ctypes.addressof(struct))
 
 
 def _kv4_here(cache, batch) -> int:

@@ -124,3 +124,29 @@ def test_batches_that_always_run(shim):
     beyond = [(1024, 1024, 65536, 65536, 1, 1), (8, 1024, 8, 65535 * 32, 64, 1 << 20)]
     for case, kernels in zip(beyond, attention_launches(shim, beyond)):
         assert len(kernels) == 1 and "too many rows" in kernels[0], (case, kernels)
+
+
+# --- handles ---------------------------------------------------------------------------------
+
+def test_handles_keep_the_tensors_they_were_made_of(monkeypatch):
+    """Another tensor in a handle's place would leave the calls with the address of the first
+    one, which nothing keeps alive any more: refused.  Its contents may change."""
+    import torch
+
+    monkeypatch.setattr(comet, "_tensor", lambda *a: None)
+    ints = lambda *v: torch.tensor(v, dtype=torch.int32)  # noqa: E731
+    b = comet.KV4Batch(ints(0, 1, 3), ints(5, 9), ints(0, 1).view(2, 1), 3)
+    codes, params = torch.zeros((4, 2, 16, 32), dtype=torch.uint8), torch.zeros((4, 2, 16, 2, 2))
+    c = comet.KV4Cache(codes, params, codes, params)
+    for handle, name, value in ((b, "seq_lens", b.seq_lens + 1), (b, "row_start", ints(0, 1, 3)),
+                                (b, "block_table", ints(0, 1).view(2, 1)), (b, "M", 2),
+                                (b, "max_rows", 1), (b, "struct", None), (c, "k_codes", codes.clone()),
+                                (c, "v_params", params.clone()), (c, "G", 64), (c, "address", 0)):
+        before = getattr(handle, name)
+        with pytest.raises(AttributeError, match=name):
+            setattr(handle, name, value)
+        assert getattr(handle, name) is before
+    lens = b.seq_lens
+    b.seq_lens.add_(1)
+    b.seq_lens += 1
+    assert b.seq_lens is lens and b.struct.seq_lens == lens.data_ptr() and lens.tolist() == [7, 11]
