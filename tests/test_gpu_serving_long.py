@@ -174,3 +174,36 @@ def test_tensors_of_a_device_that_is_not_the_current_one(monkeypatch):
             call()
     with pytest.raises(ValueError, match="x: on device 0, the current device is 1"):
         comet.rope(k, pos, freqs)
+
+
+# --- rows before the first sequence ----------------------------------------------------------
+
+@pytest.mark.parametrize("seqs,kvh,H", [([(0, 9), (1, 70), (4, 300)], 2, 8),
+                                        ([(0, 0), (70, 90), (1, 30), (64, 500)], 8, 32)])
+def test_rows_before_the_first_sequence_stay(seqs, kvh, H):
+    lead, D, G = 5, 64, 32
+    p = Paged(95 + kvh, seqs, kvh, D, G, 16)
+    cache, _ = handles(p)
+    M = lead + p.M + 2
+    batch = comet.KV4Batch(dev(p.row_start + np.int32(lead)), dev(p.lens), dev(p.table), M,
+                           max(n for n, _ in seqs))
+    new = [kv_rows(p.rng, M, kvh, D) for _ in "kv"]
+    comet.kv4_append(cache, batch, dev16(new[0]), dev16(new[1]))
+    for i in (0, 1):
+        c, prm = oracle.kv4_quantize(new[i][lead:lead + p.M].reshape(-1, D), G)
+        c, prm = c.reshape(p.M, kvh, -1), prm.reshape(p.M, kvh, D // G, 2)
+        for m, b, pos in p.rows():
+            p.store(i, b, [pos], c[m:m + 1], prm[m:m + 1])
+    assert np.array_equal(cache.k_codes.cpu().numpy(), p.codes[0])
+    assert np.array_equal(host16(cache.v_params), p.params[1])
+    marked = lambda heads: torch.full((M, heads, D), 0x1234, dtype=torch.int16,  # noqa: E731
+                                      device=DEV).view(torch.float16)
+    k, v, out = marked(kvh), marked(kvh), marked(H)
+    comet.kv4_gather(cache, batch, k_out=k, v_out=v)
+    assert np.array_equal(host16(v)[lead:-2], p.dequantized(1))
+    q16 = to16(p.rng.standard_normal((M, H, D)))
+    comet.kv4_attention(dev16(q16), cache, batch, out=out)
+    ref, bound = p.attention(q16[lead:-2], H, D ** -0.5)
+    check_attention(host16(out)[lead:-2], ref, bound)
+    for t in (k, v, out):
+        assert (host16(t)[:lead] == 0x1234).all() and (host16(t)[-2:] == 0x1234).all()
