@@ -248,7 +248,9 @@ COMET_API comet_status_t comet_rope(const uint16_t* X, const int32_t* positions,
  *           pairs floor(i(high)) and ceil(i(low)) (clamped to 0 .. rot_dim - 1,
  *           0.001 apart at least), where i(n) = rot_dim ln(original_len / (2 pi n))
  *           / (2 ln base) is where a pair makes n turns; *mscale =
- *           0.1 ln(factor) + 1 (1 for the others) (arXiv 2309.00071). */
+ *           0.1 ln(factor) + 1 (1 for the others).  The form in which checkpoints
+ *           stretched by the method of arXiv 2309.00071 are run; the paper's own
+ *           text blends by turns, which is BANDS with this *mscale. */
 typedef enum {
   COMET_ROPE_NONE = 0,
   COMET_ROPE_LINEAR = 1,
@@ -345,11 +347,15 @@ COMET_API comet_status_t comet_kv4_gather(const comet_kv4_cache_t* cache,
  * with the k_j and v_j of kv head h / (heads / kv_heads) as q * s + mn of their
  * codes, without the rounding to fp16 of comet_kv4_dequantize.  A row that sees
  * no token is zeros; one that sees a token is not-a-number where its q has an
- * infinity or not-a-number.  Products are exact to fp16 inputs (the weights w_j, and
- * those times a scale of V, are rounded to fp16, relative to the largest), sums
- * are fp32, the output is rounded once.  Scales of V below 2^-22 of the largest
- * in a sequence lose bits.  What a row does not see has no influence on it, not-a-number
- * included.  Deterministic for a given build, device and batch.
+ * infinity or not-a-number.  Products are exact to fp16 inputs, sums
+ * are fp32, the output is rounded once.  The weights w_j and those times a scale of
+ * V are rounded to fp16, relative to the row's largest weight and to the largest
+ * scale of V among the tokens that its block of rows meets, seen by the row or not:
+ * a weight keeps its 11 bits down to 2^-20 of the largest (none is left below 2^-31),
+ * a scale down to 2^-22, their product down to 2^-24.  Apart from the steps that far
+ * down, what a row does not see has no influence on it, not-a-number included.
+ * Deterministic for a given build, device and batch; how a row's tokens are split,
+ * and with that its last bits, depends on the other sequences of the batch.
  *   Q, out     device fp16, rows of `heads` heads of head_dim channels, row m at
  *              element m * q_stride (out_stride); 16-byte aligned, strides
  *              multiples of 8 and at least heads * head_dim; no overlap.

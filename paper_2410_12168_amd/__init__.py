@@ -791,7 +791,9 @@ class KV4Batch(_Handle):
     """The rows of a call and where their sequences lie: row_start int32 [B + 1], seq_lens
     int32 [B], block_table int32 [B][max_pages] (comet_kv4_batch_t), CUDA tensors that this
     object keeps alive; their contents are read when the work runs.  M: rows of the buffers;
-    max_rows: the most rows of one sequence (M if not given)."""
+    max_rows: the most rows of one sequence (M if not given).  It decides which kernels
+    kv4_attention launches: 64 single tokens without it take 3 to 4 us more a call (1024
+    tokens each, 64 heads over 8: 24.5 us, 20.7 with max_rows=1) and 65 MB more of workspace."""
 
     def __init__(self, row_start, seq_lens, block_table, M: int, max_rows: Optional[int] = None):
         for name, t in (("row_start", row_start), ("seq_lens", seq_lens),

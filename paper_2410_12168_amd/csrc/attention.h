@@ -170,7 +170,10 @@ __device__ inline uint32_t ranges_of(const SeqWork& w, float per) {
 // sum can be off), then where the unit is.  Shorter last ranges can make that more
 // units than run at once, and the device waits for a second turn of a few: ranges up
 // to half as long again are then tried (64 users of 4096 tokens, 64 heads over 8 of
-// 128 channels: 60 us without, 53 with; 32 users of up to 8192: 44 and 41).  Sums of
+// 128 channels: 60 us without, 53 with; 32 users of up to 8192: 44 and 41), with up to
+// 64 sequences, whose lengths one reading has (65 users of 1024 tokens: 28 us, 64: 21).
+// With B sequences a wave reads up to 2 B lengths, and blocks grow with B: their square
+// shows from about a thousand on (kv4_attention.hip has the times).  Sums of
 // 32 bits: more than a launch can have only in batches that the interface does not
 // allow, whose units are then any or none of the batch's.
 template <bool SPLIT>

@@ -24,8 +24,9 @@
 //     however large the scores: with the whole factor in it, a rounded maximum of 2^24
 //     and more left exponents above 0, and weights beyond fp16.
 //   - w_j s_j is scaled by a power of two per wave, so that the largest scale of
-//     the tokens so far lands in [2^14, 2^15): a weight loses bits only where it
-//     is 2^-28 of the largest.  It is rounded to fp16 (2^-11 relative).
+//     the tokens so far lands in [2^14, 2^15), or a 16th of that for odd tokens, whose
+//     codes are 16 times as large: the product loses bits only below 2^-28 (odd tokens:
+//     2^-24) of the largest.  It is rounded to fp16 (2^-11 relative).
 //   - V's operand needs 8 tokens of a channel in a lane; the cache has channels
 //     in a row.  The transposing LDS read (ds_read_b64_tr_b4: 16 rows of 16
 //     nibbles) turns 16 tokens x 16 channels at a time.
@@ -48,10 +49,12 @@
 //
 // What bounds it (64 q heads over 8 of 128 channels where nothing else is said; times
 // of a call, passes back to back, floors at the 4.9 TB/s of a large copy):
-//   - 64 users of up to 8192 tokens (284 MB): 73 us, 3.9 TB/s, floor 57.  The waves
-//     wait for the cache: each has the next tile's codes in flight, three blocks on a
-//     compute unit, and the last blocks end alone.  Two thirds or twice the token
-//     ranges run within 2%.
+//   - 64 users of up to 8192 tokens (284 MB): 73 us, 3.9 TB/s, floor 57: 4.2 TB/s in this
+//     kernel (vector operations issue in 58% of its cycles, the matrix core works in 13%),
+//     5 us for the sum over ranges.  Users of 8192 tokens each (573 MB): 109 us, 5.2 TB/s;
+//     64-channel groups 117, 32-channel ones (673 MB) 161, with more to add up per code
+//     and 7 registers spilled.  What holds the ragged batch at 4.2 is not shown; two thirds
+//     or twice the token ranges run within 2%.
 //   - one user of 131072 tokens, 32 heads (143 MB): 39 us, 3.6 TB/s, floor 29, of which
 //     the sum over 96 ranges and the launches are 8.  Fewer or more ranges: 37 us
 //     with two thirds, 44 with 4/3.
@@ -59,6 +62,10 @@
 //     the table and a tile to fetch one after the other, then the waves' sums.
 //   - 16 users with 5 drafted rows each, 12 heads of 64 channels, up to 2000 tokens:
 //     16 us (floor 3), 12 of it this kernel and 4 the sum over ranges.
+//   - many users: 65 of 8192 tokens 126 us, 128 213, 256 407 (of 1024 tokens, 64: 21, 65:
+//     28, 128: 36, 256: 67).  Every wave reads all sequences' lengths to find its unit,
+//     which grows with their square: of 200 tokens, 256 31 us (floor 13), 1024 230 (52),
+//     4096 2460 (207), 16384 35600 (830), 65536 554000 (3320).
 #include <algorithm>
 #include <cmath>
 
@@ -70,7 +77,9 @@ namespace {
 
 // ---- the products --------------------------------------------------------------
 
-// Blocks that a compute unit holds at a time, as the registers allow.
+// Blocks that a compute unit holds at a time, as the registers allow.  (With 128
+// channels in groups of 32 they do not quite: 7 are spilled with C = 1, 5 with C = 2,
+// 16 and 24 bytes a lane.)
 __host__ __device__ constexpr int resident_few(int D, int G, int C) {
   return (C == 1 ? 3 : 2) + (D == 64 && (C == 1 || G == 64) ? 1 : 0);
 }

@@ -38,11 +38,12 @@
 // last row blocks of a sequence see most tokens and come first, so that short ones
 // fill the end.
 //
-// Bound by the issue of vector operations: per wave and tile of 32 rows x 64 tokens 34
-// products, about 345 other vector operations and 32 exponentials share a SIMD's issue
-// with the second block's wave (measured: 4 products 62 ns, 32 multiply-adds 78, both
-// together 94).  Vector operations issue in 62% of the cycles, the matrix core works in
-// 38%.  A chunk of 512 rows over 16384 tokens, 64 heads of 128 channels (270 GFLOP):
+// Held by vector operations and products that hardly overlap: per wave and tile of 32
+// rows x 64 tokens 34 products, about 345 other vector operations and 32 exponentials
+// share a SIMD's issue with the second block's wave.  Vector operations issue in 61% of
+// the cycles, the matrix core works in 37%, neither of them full (in a probe, 4 products
+// took 62 ns, 32 multiply-adds 78, both together 94: side by side they could issue in
+// about 80%).  A chunk of 512 rows over 16384 tokens, 64 heads of 128 channels (270 GFLOP):
 // 349 to 361 us, 750 to 776 TFLOP/s; a large fp16 library product reaches 1307.  Prompts
 // of up to 2048 rows, four of them, 32 heads, 64-channel groups: 122 us.  Not kept, as 1
 // to 5% slower: the weights' sum by a product with a row of ones, scaling and conversion
@@ -220,8 +221,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
                  (_Float16)(v[3] * 0.0625f), (_Float16)(v[7] * 0.0625f)};
   }
   // The offsets' part of a score, sum_g mn_g (sum q)_g, is a step of the score product
-  // of its own: three fp16 numbers that add up to (sum q)_g * 2^-8 (2^-34 of the row's
-  // largest value off at most), each against mn_g.
+  // of its own: three fp16 numbers that add up to (sum q)_g * 2^-8, each against mn_g
+  // (off by 2^-33 of the sum or, where that is small, by fp16's smallest steps: 2^-27 of
+  // the row's largest value at most).
   f16x8 qsums;
   {
     f16x8 low = {0, 0, 0, 0, 0, 0, 0, 0}, high = low;  // of the halves of the lanes

@@ -11,13 +11,16 @@
 // runs of rows * head_dim / 2 bytes of codes.  Few rows: the heads are spread
 // over blocks as well.
 //
-// Bound by HBM: 2 bytes per channel on one side, 0.5 and 4 / G on the other.  Eight
-// ragged prompts of up to 4096 rows in and their contexts of up to 4596 back, 8 heads of
-// 128 channels, 32-channel groups (184 MB): 46 us for the two calls, 4.0 TB/s, of the
-// 4.9 TB/s of a large copy.  The rows of fp16 pass the caches by both ways (gather
-// with plain stores: 52 us); the codes do not, since attention reads them next
-// (append with non-temporal stores: 49 us).  16 users' single rows: 9.5 us for the two
-// calls, which is the calls.
+// 2 bytes per channel on one side, 0.5 and 4 / G on the other.  Eight ragged prompts of
+// up to 4096 rows, 8 heads of 128 channels, 32-channel groups:
+//   - append (76 MB): 25 us, 3.0 TB/s of a large copy's 4.9.  Bound by the issue of
+//     vector operations, in 95% of the cycles: the run-time sizes' divisions, reductions
+//     by lane permutes of run-time length, and two divisions a lane.
+//   - gather of contexts of up to 4596 (108 MB): 20.5 us, 5.3 TB/s: HBM, mostly writes.
+// The rows of fp16 pass the caches by both ways (both calls 46 us, with gather's plain
+// stores 52); the codes do not, since attention reads them next (with append's
+// non-temporal stores 49).  16 users' single rows: 9 to 10 us for the two calls, which
+// is the calls.
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
 #include <stdint.h>
