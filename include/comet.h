@@ -347,8 +347,9 @@ COMET_API comet_status_t comet_kv4_gather(const comet_kv4_cache_t* cache,
  * with the k_j and v_j of kv head h / (heads / kv_heads) as q * s + mn of their
  * codes, without the rounding to fp16 of comet_kv4_dequantize.  A row that sees
  * no token is zeros; one that sees a token is not-a-number where its q has an
- * infinity or not-a-number.  Products are exact to fp16 inputs, sums
- * are fp32, the output is rounded once.  The weights w_j and those times a scale of
+ * infinity or not-a-number.  Products are exact to fp16 inputs (but
+ * for channels of q below 2^-24 of the row's largest, which lose bits), sums are fp32,
+ * the output is rounded once.  The weights w_j and those times a scale of
  * V are rounded to fp16, relative to the row's largest weight and to the largest
  * scale of V among the tokens that its block of rows meets, seen by the row or not:
  * a weight keeps its 11 bits down to 2^-20 of the largest (none is left below 2^-31),

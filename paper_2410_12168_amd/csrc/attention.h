@@ -23,6 +23,9 @@ constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kNone = -1e30f;  // maximum of no scores
 constexpr int kTile = 64;        // tokens a wave takes at a time
 constexpr int kWaves = 4;
+// q is scaled so that a row's largest value lies in [2^kQueryBits, 2^(kQueryBits + 1)): as
+// far up as fp16 goes, since small channels reach its lower end (odd ones a 16th of that)
+constexpr int kQueryBits = 14;
 // fewest tiles in a range: one for each wave
 constexpr int kMinTiles = kWaves;
 

@@ -16,8 +16,9 @@
 //     two masks and a shift make eight of them from a dword, every second one
 //     16 times larger (its nibble sits four bits higher), which the other
 //     operand takes back.  The order within a dword is (0, 4, 1, 5, 2, 6, 3, 7).
-//   - q is scaled by a power of two per row (largest value in [2^10, 2^11)), so
-//     that neither that factor nor subnormals cost bits.
+//   - q is scaled by a power of two per row (largest value in [2^14, 2^15)): the factor
+//     costs no bits, subnormals cost some from 2^-24 of the largest value down (2^-35 of
+//     it at most).  With the largest in [2^10, 2^11) it was from 2^-20 on.
 //   - scale * log2(e) is a mantissa, multiplied into K's scales and the sums of q, times
 //     a power of two that turns a score into the exponent of its weight (`kappa`).  That
 //     product is exact, so that the largest score's exponent is 0 and none is above it,
@@ -236,13 +237,13 @@ __global__ __launch_bounds__(64 * kWaves, resident_few(D, G, C)) void kv4_attent
         big = fmaxf(big, fmaxf(fabsf(low_half(raw[s][k])), fabsf(low_half(raw[s][k] >> 16))));
     }
     big = quad_max(big);
-    int e = 10;
+    int e = kQueryBits;
     if (big > 0.0f && big < INFINITY) e = ilogbf(big);
     // an infinity in q: all scores of the row are infinities or not-a-numbers, and its
     // weights not-a-numbers, whatever their sign
-    const float f = big < INFINITY ? ldexpf(a.scale < 0.0f ? -1.0f : 1.0f, 10 - e) : NAN;
+    const float f = big < INFINITY ? ldexpf(a.scale < 0.0f ? -1.0f : 1.0f, kQueryBits - e) : NAN;
     // above 0, so that an unseen token's -infinity stays one
-    kappa[cb] = fmaxf(ldexpf(1.0f, a.exponent + 24 + e - 10), 0x1p-120f);
+    kappa[cb] = fmaxf(ldexpf(1.0f, a.exponent + 24 + e - kQueryBits), 0x1p-120f);
     #pragma unroll
     for (int g = 0; g < NG; ++g) qsum[cb][g] = 0.0f;
     #pragma unroll

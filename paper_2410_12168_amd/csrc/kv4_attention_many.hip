@@ -196,12 +196,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
     for (int k = 0; k < 4; ++k)
       big = fmaxf(big, fmaxf(fabsf(low_half(raw[s][k])), fabsf(low_half(raw[s][k] >> 16))));
   big = pair_max(big);
-  int e = 10;
+  int e = kQueryBits;
   if (big > 0.0f && big < INFINITY) e = ilogbf(big);
   // an infinity in q makes the row not-a-number (see kv4_attention.hip)
-  const float qf = big < INFINITY ? ldexpf(a.scale < 0.0f ? -1.0f : 1.0f, 10 - e) : NAN;
+  const float qf = big < INFINITY ? ldexpf(a.scale < 0.0f ? -1.0f : 1.0f, kQueryBits - e) : NAN;
   // above 0, so that an unseen token's -infinity stays one
-  const float kappa = fmaxf(ldexpf(1.0f, a.exponent + 8 + e - 10), 0x1p-120f);
+  const float kappa = fmaxf(ldexpf(1.0f, a.exponent + 8 + e - kQueryBits), 0x1p-120f);
   #pragma unroll
   for (int g = 0; g < NG; ++g) qsum[g] = offset[g] = eights[g] = 0.0f;
   #pragma unroll
@@ -222,7 +222,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv4_attention_many_kernel(
   }
   // The offsets' part of a score, sum_g mn_g (sum q)_g, is a step of the score product
   // of its own: three fp16 numbers that add up to (sum q)_g * 2^-8, each against mn_g
-  // (off by 2^-33 of the sum or, where that is small, by fp16's smallest steps: 2^-27 of
+  // (off by 2^-33 of the sum or, where that is small, by fp16's smallest steps: 2^-30 of
   // the row's largest value at most).
   f16x8 qsums;
   {
