@@ -207,3 +207,36 @@ def test_rows_before_the_first_sequence_stay(seqs, kvh, H):
     check_attention(host16(out)[lead:-2], ref, bound)
     for t in (k, v, out):
         assert (host16(t)[:lead] == 0x1234).all() and (host16(t)[-2:] == 0x1234).all()
+
+
+# --- one quantizer in two kernels ------------------------------------------------------------
+
+@pytest.mark.parametrize("D,G", FORMS)
+def test_append_quantizes_as_the_flat_quantizer_does(D, G):
+    """Rows of any finite fp16 bits, of all exponents and of few, constants and ties: the codes
+    and parameters of comet_kv4_quantize, bit for bit."""
+    rng = np.random.default_rng(D + G)
+    M, kvh, page = 4096, 3, 64
+    rows = rng.integers(0, 1 << 16, (M, kvh, D)).astype(np.uint16)
+    rows[(rows & 0x7C00) == 0x7C00] ^= 0x4000  # finite
+    rows[M // 4:M // 2] &= 0x83FF  # subnormals
+    rows[M // 2:3 * M // 4] = to16(rng.integers(-8, 9, (M // 4, kvh, D)) * 2.0 ** rng.integers(
+        -20, 12, (M // 4, kvh, 1)))  # multiples of a power of two
+    rows[-64:] = rows[-64:, :, :1]  # constant rows
+    table = rng.permutation(M // page).astype(np.int32)
+    cache = comet.KV4Cache.empty(M // page, page, kvh, D, G=G)
+    ints = lambda *a: dev(np.array(a, np.int32))  # noqa: E731
+    batch = comet.KV4Batch(ints(0, M), ints(M), dev(table[None]), M)
+    x = dev16(rows)
+    comet.kv4_append(cache, batch, x, x)
+    codes, params = comet.kv4_quantize(x.view(M * kvh, D), G=G)
+    want = codes.view(M // page, page, kvh, D // 2).transpose(1, 2)
+    want_params = params.view(M // page, page, kvh, D // G, 2).transpose(1, 2)
+    at = dev(table).long()
+    for c, prm in ((cache.k_codes, cache.k_params), (cache.v_codes, cache.v_params)):
+        assert torch.equal(c[at], want)
+        assert torch.equal(prm[at].view(torch.int16), want_params.contiguous().view(torch.int16))
+    k, v = comet.kv4_gather(cache, batch)
+    flat = comet.kv4_dequantize(codes, params, G=G).view(M, kvh, D)
+    assert torch.equal(k.view(torch.int16), flat.view(torch.int16))
+    assert torch.equal(v.view(torch.int16), flat.view(torch.int16))
